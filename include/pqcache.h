@@ -66,7 +66,7 @@ typedef enum pqc_status {
                          * than the library's static array holds                     */
 } pqc_status;
 
-typedef enum pqc_dtype { PQC_F32 = 0, PQC_BF16 = 1 } pqc_dtype;
+typedef enum pqc_dtype { PQC_F32 = 0, PQC_BF16 = 1, PQC_FP8 = 2 /* e4m3, pages only */ } pqc_dtype;
 
 /* Shape of one decode step.  Supported: head_dim = 128; pq_m in {1,2,4,8};
  * 1 <= pq_centroids <= 256; n_q_heads / n_kv_heads in {1,2,4,8};
@@ -355,6 +355,112 @@ int pqc_block_cache_update(const pqc_config* cfg, int32_t block_tokens, int32_t 
                            int32_t step, const int32_t* counts, const int32_t* blocks, int32_t k_cache,
                            int32_t* slot_block, int32_t* slot_stamp, int32_t* slot_uses, int32_t* stats,
                            void* stream);
+
+/* ---- a paged key/value cache: ragged sequences, rows of 16 or 8 bits ----
+ *
+ * Keys and values of all sequences lie in pages of page_tokens tokens of one pool; a page
+ * table names the pages of each sequence in order, so that sequences of any length share the
+ * memory and grow without being moved.  Per decode step a program appends the new tokens and
+ * attends: to all tokens (pqc_paged_attn), or to those that a retrieval step selected
+ * (pqc_lut, pqc_scan, pqc_topk, whose out_idx pqc_paged_gather_attn takes).
+ *
+ *   k_pages, v_pages  [n_pages][Hkv][page_tokens][D]  cache_dtype
+ *   k_scale, v_scale  [n_pages][Hkv] f32   PQC_FP8 only (else ignored, may be NULL): a row's
+ *                                          values are code * scale of its page and head
+ *   page_table        [B][max_pages] int32 pages of sequence b; an entry outside
+ *                                          [0, n_pages) is a page that is not there: nothing
+ *                                          is written to it and none of its tokens attended
+ *   lengths           [B] int32            tokens of each sequence, the ones that a call
+ *                                          appends or queries with included; taken into
+ *                                          [0, max_pages * page_tokens]
+ *
+ * The calls need no context, allocate nothing and synchronise nothing; the lengths, offsets
+ * and page tables are read on the device, so that a call recorded into a HIP graph follows
+ * their values from replay to replay.  What a pool holds beyond its sequences' tokens is
+ * never attended, whatever it is (NaN included).
+ * Several tokens per sequence: `offsets` [B+1] int32, ascending, within [0, n]; sequence b has
+ * the tokens offsets[b] .. offsets[b+1]-1 of the n in the call, which are the last ones of its
+ * `lengths[b]`.  Rows outside all sequences are neither read nor written.  NULL offsets: one
+ * token per sequence (n == B).
+ * Supported: head_dim 64 or 128; up to 16 query heads per KV head, any number; page_tokens
+ * 16, 32, 64, 128 or 256; cache_dtype PQC_BF16 or PQC_FP8; max_pages * page_tokens <= 2^24;
+ * n_pages * Hkv * page_tokens < 2^31; B, Hkv <= 65535; n * Hq < 2^31. */
+typedef struct pqc_paged_config {
+  int32_t batch;         /* B                                                        */
+  int32_t n_q_heads;     /* Hq                                                       */
+  int32_t n_kv_heads;    /* Hkv, divides Hq                                          */
+  int32_t head_dim;      /* D                                                        */
+  int32_t page_tokens;
+  int32_t n_pages;       /* pages of the pool                                        */
+  int32_t max_pages;     /* entries of a sequence's row of the page table            */
+  int32_t io_dtype;      /* of q, k, v and the rotated copies: PQC_F32 or PQC_BF16   */
+  int32_t cache_dtype;   /* of the pages: PQC_BF16 or PQC_FP8                        */
+  int32_t out_dtype;     /* of the attention output: PQC_F32 or PQC_BF16             */
+  float softmax_scale;   /* factor on q.k before softmax; <= 0 means 1/sqrt(D)       */
+  int32_t rot_dims;      /* rotated dimensions of a head: a multiple of 16 up to D, 0: none */
+  int32_t rot_style;     /* PQC_ROT_HALVES or PQC_ROT_PAIRS                          */
+  int32_t rot_positions; /* rows of the rotation table                               */
+} pqc_paged_config;
+
+typedef struct pqc_paged_cache { /* device pointers, 16-byte aligned (page_table, lengths: 4) */
+  void* k_pages;
+  void* v_pages;
+  float* k_scale;
+  float* v_scale;
+  const int32_t* page_table;
+  const int32_t* lengths;
+} pqc_paged_cache;
+
+#define PQC_ROT_HALVES 0 /* dimension j is rotated with j + rot_dims/2  */
+#define PQC_ROT_PAIRS 1  /* dimension 2j is rotated with 2j + 1         */
+
+/* New tokens join the cache, their keys (and queries) rotated by position on the way:
+ *   (x1, x2) -> (x1 cos - x2 sin, x2 cos + x1 sin), products and sums in fp32.
+ *   q  [n][Hq][D], k, v [n][Hkv][D]  io_dtype; a token's heads are adjacent, tokens are
+ *       q_stride, k_stride, v_stride values apart (multiples of 8, at least heads * D: the
+ *       three may be parts of the rows of one projection).  q may be NULL.
+ *   rotation   [rot_positions][rot_dims] f32   per position cos of the rot_dims/2 angles, then
+ *                                              sin; NULL with rot_dims == 0
+ *   positions  [n] int32   row of the table for each token, taken into it; NULL: the token's
+ *                          place in its sequence
+ *   q_out      [n][Hq][D]  rotated queries (required with q), k_out [n][Hkv][D] rotated keys
+ *                          (may be NULL; for pqc_pq_build, pqc_pq_encode_token): io_dtype,
+ *                          not overlapping the inputs
+ * A token goes to place lengths[b] - (tokens of b) + i of its sequence; places outside
+ * [0, max_pages * page_tokens) are not stored.  The pages written to must be of one sequence each.
+ * PQC_FP8: the scale of a (page, head), of keys and of values apart, is the smallest power of two
+ * with which all its values are within the type's 448.  If a page's scale has to grow for new
+ * tokens, its older codes are encoded anew, which a power of two leaves exact down to the
+ * type's subnormals.  A page that receives its first token starts anew, whatever it held. */
+int pqc_paged_append(const pqc_paged_config* cfg, const pqc_paged_cache* cache, const void* q, int64_t q_stride,
+                     const void* k, int64_t k_stride, const void* v, int64_t v_stride, int32_t n,
+                     const int32_t* offsets, const int32_t* positions, const float* rotation, void* q_out,
+                     void* k_out, void* stream);
+
+/* Bytes of device workspace of the two attention calls below, for n query tokens over all
+ * sequences and, for pqc_paged_gather_attn, n_idx listed tokens per head (0 for
+ * pqc_paged_attn).  Of the configuration's sizes alone, not of what the arrays hold.  0 if the
+ * configuration is refused, and where no workspace is needed. */
+size_t pqc_paged_workspace_bytes(const pqc_paged_config* cfg, int32_t n, int32_t n_idx);
+
+/* Softmax attention of every query head over all cached tokens of its sequence up to the
+ * query's own place (causal): query token i of the m of sequence b sees the tokens
+ * t <= lengths[b] - m + i.  A query that sees none gives zeros.
+ *   q    [n][Hq][D] io_dtype     out  [n][Hq][D] out_dtype
+ *   workspace  256-byte aligned, pqc_paged_workspace_bytes(cfg, n, 0); contents need not be
+ *              kept, calls that share it must be ordered on one stream
+ * Sums, maxima and softmax weights are fp32; the weights enter the product with the values in
+ * two bf16 terms for an fp32 output (2^-18 of a weight left out). */
+int pqc_paged_attn(const pqc_paged_config* cfg, const pqc_paged_cache* cache, const void* q, int32_t n,
+                   const int32_t* offsets, void* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The same for one query token per sequence over listed tokens only: idx [B][Hkv][n_idx] int32
+ * (as out_idx of pqc_topk or pqc_decode), shared by the query heads of a KV head.  Entries
+ * outside [0, lengths[b]) are left out, so that lists of different lengths can be padded with -1;
+ * a token listed twice counts twice.  q [B][Hq][D], out [B][Hq][D]; a head without tokens gives
+ * zeros.  Workspace: pqc_paged_workspace_bytes(cfg, B, n_idx). */
+int pqc_paged_gather_attn(const pqc_paged_config* cfg, const pqc_paged_cache* cache, const void* q, const int32_t* idx,
+                          int32_t n_idx, void* out, void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -1,0 +1,221 @@
+// C entry points of the paged key/value cache: checks, launch shapes and dispatch.  Nothing allocates or synchronises.
+#include "../../include/pqcache.h"
+
+#include <algorithm>
+#include <cmath>
+
+#include "pqc_paged_kernels.h"
+
+namespace {
+
+using namespace pqc;
+using namespace pqc::paged;
+
+bool aligned(const void* p, unsigned n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+// Items per head that the length of a split aims at: about two workgroups of four waves per compute unit over all heads.
+constexpr int kItems = 512;
+
+int make_geometry(const pqc_paged_config* c, long long n, Geometry* g) {
+  if (!c) return PQC_EINVAL;
+  if (c->batch < 1 || c->n_q_heads < 1 || c->n_kv_heads < 1 || c->n_q_heads % c->n_kv_heads || c->head_dim < 1 || c->page_tokens < 1 ||
+      c->n_pages < 1 || c->max_pages < 1 || n < 0)
+    return PQC_EINVAL;
+  if (c->io_dtype != PQC_F32 && c->io_dtype != PQC_BF16) return PQC_EINVAL;
+  if (c->out_dtype != PQC_F32 && c->out_dtype != PQC_BF16) return PQC_EINVAL;
+  if (c->cache_dtype != PQC_F32 && c->cache_dtype != PQC_BF16 && c->cache_dtype != PQC_FP8) return PQC_EINVAL;
+  if (!std::isfinite(c->softmax_scale)) return PQC_EINVAL;
+  if (c->rot_dims < 0 || c->rot_dims > c->head_dim || (c->rot_dims && c->rot_positions < 1)) return PQC_EINVAL;
+  if (c->rot_style != PQC_ROT_HALVES && c->rot_style != PQC_ROT_PAIRS) return PQC_EINVAL;
+  const int G = c->n_q_heads / c->n_kv_heads, P = c->page_tokens;
+  if (c->head_dim != 64 && c->head_dim != 128) return PQC_EUNSUPPORTED;
+  if (G > kRows || c->cache_dtype == PQC_F32 || c->rot_dims % 16) return PQC_EUNSUPPORTED;
+  if (P < 16 || P > 256 || (P & (P - 1))) return PQC_EUNSUPPORTED;
+  if (c->batch > 65535 || c->n_kv_heads > 65535) return PQC_EUNSUPPORTED;
+  if ((long long)c->max_pages * P > (1 << 24) || (long long)c->n_pages * c->n_kv_heads * P >= (1ll << 31)) return PQC_EUNSUPPORTED;
+  if (n * c->n_q_heads >= (1ll << 31)) return PQC_EUNSUPPORTED;
+  g->B = c->batch; g->Hq = c->n_q_heads; g->Hkv = c->n_kv_heads; g->G = G;
+  g->P = P;
+  g->shift = __builtin_ctz((unsigned)P);
+  g->n_pages = c->n_pages; g->max_pages = c->max_pages;
+  g->n_q = (int)n;
+  g->R = kRows / G;
+  g->out_bf16 = c->out_dtype == PQC_BF16;
+  const float scale = c->softmax_scale > 0.0f ? c->softmax_scale : 1.0f / std::sqrt((float)c->head_dim);
+  g->scale_log2e = scale * 1.4426950408889634f;
+  g->per_head = std::max(1, (kItems + g->Hkv - 1) / g->Hkv);
+  g->items = g->slots = g->split = g->n_split = 0;
+  return PQC_OK;
+}
+
+// Bounds of the items and of the partial results of a call with (at most) one or several query tokens per sequence.
+void plan_attn(Geometry* g, bool one_each) {
+  if (one_each) g->R = 1;
+  const int tiles = one_each ? g->B : (int)std::min<long long>(g->n_q, (long long)g->n_q / g->R + g->B);
+  g->items = tiles + g->per_head;
+  g->slots = 2 * g->per_head;
+}
+// Listed tokens: the splits of a sequence are as many as give the items of all sequences the number aimed at.
+void plan_listed(Geometry* g, int n_idx) {
+  g->R = 1;
+  const long long most = std::max(1, g->per_head / g->B);
+  g->split = (int)(((n_idx + most - 1) / most + kGrain - 1) / kGrain) * kGrain;
+  g->split = std::max(g->split, kGrain);
+  g->n_split = std::max(1, (n_idx + g->split - 1) / g->split);
+  g->slots = g->n_split > 1 ? g->B * g->n_split : 0;
+}
+size_t partial_bytes(const Geometry& g, int head_dim) {
+  return ((size_t)g.slots * g.Hkv * g.R * g.G * (head_dim + 2) * sizeof(float) + 255) / 256 * 256;
+}
+
+int check_cache(const pqc_paged_config* cfg, const pqc_paged_cache* c) {
+  if (!c || !c->k_pages || !c->v_pages || !c->page_table || !c->lengths) return PQC_EINVAL;
+  if (cfg->cache_dtype == PQC_FP8 && (!c->k_scale || !c->v_scale)) return PQC_EINVAL;
+  if (!aligned(c->k_pages, 16) || !aligned(c->v_pages, 16) || !aligned(c->page_table, 4) || !aligned(c->lengths, 4)) return PQC_EINVAL;
+  if (cfg->cache_dtype == PQC_FP8 && (!aligned(c->k_scale, 16) || !aligned(c->v_scale, 16))) return PQC_EINVAL;
+  return PQC_OK;
+}
+Cache device_cache(const pqc_paged_cache* c) {
+  return Cache{static_cast<unsigned char*>(c->k_pages), static_cast<unsigned char*>(c->v_pages), c->k_scale, c->v_scale, c->page_table, c->lengths};
+}
+int launched() { return hipGetLastError() == hipSuccess ? PQC_OK : PQC_EHIP; }
+
+struct AttnCall {
+  const Geometry& g;
+  const Cache& c;
+  const void* q;
+  const int* offsets;
+  const int* idx;
+  int n_idx;
+  void* out;
+  float* partials;
+  hipStream_t st;
+};
+template <typename T, class C, int D, bool LISTED>
+void launch_rows(const AttnCall& a) {
+  const Geometry& g = a.g;
+  const unsigned items = LISTED ? (unsigned)(g.B * g.n_split) : (unsigned)g.items;
+  hipLaunchKernelGGL((attn_rows_kernel<T, C, D, LISTED>), dim3(items, g.Hkv), dim3(256), 0, a.st, g, a.c, static_cast<const T*>(a.q), a.offsets, a.idx,
+                     a.n_idx, a.out, a.partials);
+  // tiles of several splits have two items at least
+  const unsigned split_tiles = LISTED ? (unsigned)g.B : (unsigned)std::min(g.per_head, g.items - g.per_head);
+  if (LISTED ? g.n_split > 1 : (g.max_pages << g.shift) > kGrain)
+    hipLaunchKernelGGL((attn_merge_kernel<D, LISTED>), dim3(split_tiles, g.Hkv, LISTED ? g.G : g.R * g.G), dim3(256), 0, a.st, g, a.c.lengths,
+                       a.offsets, a.partials, a.out);
+}
+template <bool LISTED>
+int launch_attn(const pqc_paged_config* cfg, const AttnCall& a) {
+  auto by_dim = [&](auto t, auto c) {
+    if (cfg->head_dim == 128)
+      launch_rows<decltype(t), decltype(c), 128, LISTED>(a);
+    else
+      launch_rows<decltype(t), decltype(c), 64, LISTED>(a);
+  };
+  const bool f32 = cfg->io_dtype == PQC_F32, fp8 = cfg->cache_dtype == PQC_FP8;
+  if (f32 && fp8) by_dim(float{}, Fp8{});
+  else if (f32) by_dim(float{}, Bf16{});
+  else if (fp8) by_dim(bf16_t{}, Fp8{});
+  else by_dim(bf16_t{}, Bf16{});
+  return launched();
+}
+
+template <typename T, bool FP8, int D>
+void launch_append(const Geometry& g, const Cache& c, const AppendArgs& a, const int* offsets, hipStream_t st) {
+  const unsigned q_groups = a.q ? (unsigned)((g.n_q + a.q_tokens - 1) / a.q_tokens) : 0;
+  hipLaunchKernelGGL((append_kernel<T, FP8, D>), dim3((unsigned)a.kv_items * 2 * g.Hkv + q_groups), dim3(256), 0, st, g, c, a, offsets);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t pqc_paged_workspace_bytes(const pqc_paged_config* cfg, int32_t n, int32_t n_idx) {
+  Geometry g;
+  if (n_idx < 0 || make_geometry(cfg, n, &g) != PQC_OK) return 0;
+  if (n_idx > 0)
+    plan_listed(&g, n_idx);
+  else
+    plan_attn(&g, false);
+  return partial_bytes(g, cfg->head_dim);
+}
+
+int pqc_paged_attn(const pqc_paged_config* cfg, const pqc_paged_cache* cache, const void* q, int32_t n, const int32_t* offsets, void* out,
+                   void* workspace, size_t workspace_bytes, void* stream) {
+  Geometry g;
+  int rc = make_geometry(cfg, n, &g);
+  if (rc != PQC_OK) return rc;
+  rc = check_cache(cfg, cache);
+  if (rc != PQC_OK) return rc;
+  if (!q || !out || !aligned(q, 16) || !aligned(out, 16) || !aligned(offsets, 4) || (!offsets && n != g.B)) return PQC_EINVAL;
+  plan_attn(&g, false);
+  const size_t need = partial_bytes(g, cfg->head_dim);
+  if (!offsets) plan_attn(&g, true);
+  if (!workspace || !aligned(workspace, 256) || workspace_bytes < need) return PQC_EWORKSPACE;
+  if (n == 0) return PQC_OK;
+  const Cache c = device_cache(cache);
+  return launch_attn<false>(cfg, AttnCall{g, c, q, offsets, nullptr, 0, out, static_cast<float*>(workspace), static_cast<hipStream_t>(stream)});
+}
+
+int pqc_paged_gather_attn(const pqc_paged_config* cfg, const pqc_paged_cache* cache, const void* q, const int32_t* idx, int32_t n_idx, void* out,
+                          void* workspace, size_t workspace_bytes, void* stream) {
+  Geometry g;
+  int rc = make_geometry(cfg, cfg ? cfg->batch : 0, &g);
+  if (rc != PQC_OK) return rc;
+  rc = check_cache(cfg, cache);
+  if (rc != PQC_OK) return rc;
+  if (!q || !out || !idx || n_idx < 1 || !aligned(q, 16) || !aligned(out, 16) || !aligned(idx, 4)) return PQC_EINVAL;
+  if (n_idx > (1 << 24)) return PQC_EUNSUPPORTED;
+  plan_listed(&g, n_idx);
+  const size_t need = partial_bytes(g, cfg->head_dim);
+  if (need && (!workspace || !aligned(workspace, 256) || workspace_bytes < need)) return PQC_EWORKSPACE;
+  const Cache c = device_cache(cache);
+  return launch_attn<true>(cfg, AttnCall{g, c, q, nullptr, idx, n_idx, out, static_cast<float*>(workspace), static_cast<hipStream_t>(stream)});
+}
+
+int pqc_paged_append(const pqc_paged_config* cfg, const pqc_paged_cache* cache, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                     const void* v, int64_t v_stride, int32_t n, const int32_t* offsets, const int32_t* positions, const float* rotation, void* q_out,
+                     void* k_out, void* stream) {
+  Geometry g;
+  int rc = make_geometry(cfg, n, &g);
+  if (rc != PQC_OK) return rc;
+  rc = check_cache(cfg, cache);
+  if (rc != PQC_OK) return rc;
+  const int64_t q_row = (int64_t)g.Hq * cfg->head_dim, kv_row = (int64_t)g.Hkv * cfg->head_dim;
+  if (!k || !v || (q && !q_out) || (cfg->rot_dims && !rotation) || (!offsets && n != g.B)) return PQC_EINVAL;
+  if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(q_out, 16) || !aligned(k_out, 16) || !aligned(rotation, 16) ||
+      !aligned(offsets, 4) || !aligned(positions, 4))
+    return PQC_EINVAL;
+  if (k_stride < kv_row || v_stride < kv_row || k_stride % 8 || v_stride % 8 || (q && (q_stride < q_row || q_stride % 8))) return PQC_EINVAL;
+  // a value's partner may be read after it was overwritten
+  if ((q && q_out == q) || (k_out && (k_out == k || k_out == v || k_out == q || k_out == q_out))) return PQC_EINVAL;
+  if (n == 0) return PQC_OK;
+  AppendArgs a;
+  a.q = q; a.k = k; a.v = v;
+  a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride;
+  a.positions = positions;
+  a.table = rotation;
+  a.rot = cfg->rot_dims; a.rot_positions = cfg->rot_positions;
+  a.pairs = cfg->rot_style == PQC_ROT_PAIRS;
+  a.q_out = q_out; a.k_out = k_out;
+  a.q_tokens = n > 4096 ? 4 : 1;
+  // a sequence of m tokens touches at most 1 + (m + P - 2) / P pages, and no more than m
+  const long long pages = offsets ? std::min<long long>(n, (long long)n / g.P + 2ll * g.B) : n;
+  if (pages * 2 * g.Hkv + n >= (1ll << 31)) return PQC_EUNSUPPORTED;
+  a.kv_items = (int)pages;
+  const Cache c = device_cache(cache);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  auto by_dim = [&](auto t, auto fp8) {
+    if (cfg->head_dim == 128)
+      launch_append<decltype(t), decltype(fp8)::value, 128>(g, c, a, offsets, st);
+    else
+      launch_append<decltype(t), decltype(fp8)::value, 64>(g, c, a, offsets, st);
+  };
+  const bool f32 = cfg->io_dtype == PQC_F32, fp8 = cfg->cache_dtype == PQC_FP8;
+  if (f32 && fp8) by_dim(float{}, std::true_type{});
+  else if (f32) by_dim(float{}, std::false_type{});
+  else if (fp8) by_dim(bf16_t{}, std::true_type{});
+  else by_dim(bf16_t{}, std::false_type{});
+  return launched();
+}
+
+}  // extern "C"

@@ -1,0 +1,206 @@
+"""Paged key/value cache: ctypes marshalling over the pqc_paged_* calls of include/pqcache.h.
+
+A `PagedCache` is a view of a pool of pages that the caller owns: which sequences lie in it, and where, comes with every
+call as a page table and lengths, so that one object serves a batch that changes from step to step.  Workspaces are
+allocated per call from torch's caching allocator, hence two streams, or two captured graphs, share none.
+"""
+from __future__ import annotations
+
+import ctypes as C
+from typing import Optional, Tuple
+
+import torch
+
+from . import binding
+from .binding import PQCacheError
+
+_DTYPES = {"f32": (0, torch.float32), "bf16": (1, torch.bfloat16), "fp8": (2, torch.float8_e4m3fn)}
+_STYLES = {"halves": 0, "pairs": 1}
+
+
+class Config(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("batch", "n_q_heads", "n_kv_heads", "head_dim", "page_tokens", "n_pages", "max_pages",
+                                         "io_dtype", "cache_dtype", "out_dtype")] + [("softmax_scale", C.c_float)] + [
+                                             (n, C.c_int32) for n in ("rot_dims", "rot_style", "rot_positions")]
+
+
+class Pages(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k_pages", "v_pages", "k_scale", "v_scale", "page_table", "lengths")]
+
+
+_lib = None
+
+
+def _load():
+    global _lib
+    if _lib is None:
+        lib = binding.load()
+        vp, cfg, pages, i32, i64, size = C.c_void_p, C.POINTER(Config), C.POINTER(Pages), C.c_int32, C.c_int64, C.c_size_t
+        lib.pqc_paged_append.restype = C.c_int
+        lib.pqc_paged_append.argtypes = [cfg, pages, vp, i64, vp, i64, vp, i64, i32, vp, vp, vp, vp, vp, vp]
+        lib.pqc_paged_workspace_bytes.restype = size
+        lib.pqc_paged_workspace_bytes.argtypes = [cfg, i32, i32]
+        lib.pqc_paged_attn.restype = C.c_int
+        lib.pqc_paged_attn.argtypes = [cfg, pages, vp, i32, vp, vp, vp, size, vp]
+        lib.pqc_paged_gather_attn.restype = C.c_int
+        lib.pqc_paged_gather_attn.argtypes = [cfg, pages, vp, vp, i32, vp, vp, size, vp]
+        _lib = lib
+    return _lib
+
+
+def rotation_table(n_positions: int, rot_dims: int, base: float = 10000.0, device="cuda:0") -> torch.Tensor:
+    """[n_positions][rot_dims] f32: cosines, then sines, of position * base^(-2j / rot_dims); angles in double precision."""
+    j = torch.arange(0, rot_dims, 2, device=device, dtype=torch.float64)
+    angle = torch.arange(n_positions, device=device, dtype=torch.float64)[:, None] * base ** (-j / rot_dims)
+    return torch.cat([angle.cos(), angle.sin()], 1).to(torch.float32).contiguous()
+
+
+class PagedCache:
+    """Pages [n_pages][Hkv][page_tokens][D] of keys and of values, float8_e4m3fn with scales [n_pages][Hkv] f32, or bfloat16
+    (scales None).  Like a decode context it is not thread-safe.  `dtype`: "f32" or "bf16", of q, k and v; `out_dtype`: of the attention output; `rotation`: the table of
+    rotation_table() or one laid out like it, None for no rotation."""
+
+    def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, k_scale: Optional[torch.Tensor], v_scale: Optional[torch.Tensor], *,
+                 n_q_heads: int, dtype: str = "bf16", out_dtype: str = "f32", softmax_scale: float = 0.0,
+                 rotation: Optional[torch.Tensor] = None, rot_style: str = "halves"):
+        self.lib = _load()
+        self.device = k_pages.device
+        if k_pages.dim() != 4 or k_pages.dtype not in (torch.float8_e4m3fn, torch.bfloat16):
+            raise ValueError("pages are [n_pages][Hkv][page_tokens][D] of float8_e4m3fn or bfloat16")
+        n_pages, heads, tokens, dim = k_pages.shape
+        self.io = _DTYPES[dtype][1]
+        self.out = _DTYPES[out_dtype][1]
+        self.k_pages, self.v_pages, self.k_scale, self.v_scale, self.rotation = k_pages, v_pages, k_scale, v_scale, rotation
+        self._need(k_pages, k_pages.dtype, k_pages.shape, "k_pages")
+        self._need(v_pages, k_pages.dtype, k_pages.shape, "v_pages")
+        fp8 = k_pages.dtype is torch.float8_e4m3fn
+        if fp8:
+            self._need(k_scale, torch.float32, (n_pages, heads), "k_scale")
+            self._need(v_scale, torch.float32, (n_pages, heads), "v_scale")
+        rot_dims = rot_positions = 0
+        if rotation is not None:
+            rot_positions, rot_dims = rotation.shape
+            self._need(rotation, torch.float32, rotation.shape, "rotation")
+        self.heads, self.dim, self.q_heads = heads, dim, n_q_heads
+        self.cfg = Config(1, n_q_heads, heads, dim, tokens, n_pages, 1, _DTYPES[dtype][0], 2 if fp8 else 1, _DTYPES[out_dtype][0],
+                          softmax_scale, rot_dims, _STYLES[rot_style], rot_positions)
+        self.pages = Pages(k_pages.data_ptr(), v_pages.data_ptr(), k_scale.data_ptr() if fp8 else None,
+                           v_scale.data_ptr() if fp8 else None, None, None)
+        self._cfg, self._pages = C.byref(self.cfg), C.byref(self.pages)
+
+    @classmethod
+    def empty(cls, n_pages: int, n_q_heads: int, n_kv_heads: int, head_dim: int = 128, page_tokens: int = 64, cache_dtype: str = "fp8",
+              device="cuda:0", **more) -> "PagedCache":
+        """A cache with a pool of its own."""
+        shape = (n_pages, n_kv_heads, page_tokens, head_dim)
+        k, v = (torch.empty(shape, dtype=_DTYPES[cache_dtype][1], device=device) for _ in range(2))
+        ks = vs = None
+        if cache_dtype == "fp8":
+            ks, vs = (torch.ones((n_pages, n_kv_heads), dtype=torch.float32, device=device) for _ in range(2))
+        return cls(k, v, ks, vs, n_q_heads=n_q_heads, **more)
+
+    # -- marshalling helpers
+    def _need(self, t, dtype, shape, what: str) -> int:
+        if t is None or t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.device != self.device:
+            got = "None" if t is None else f"{t.dtype} {tuple(t.shape)} on {t.device}"
+            raise ValueError(f"{what}: expected contiguous {dtype} {tuple(shape)} on {self.device}, got {got}")
+        return t.data_ptr()
+
+    def _rows(self, t: torch.Tensor, n: int, heads: int, what: str) -> Tuple[int, int]:
+        """Address and token stride of [n][heads][D] whose heads are adjacent."""
+        if t.dtype is not self.io or t.shape != (n, heads, self.dim) or t.device != self.device:
+            raise ValueError(f"{what}: expected {self.io} {(n, heads, self.dim)} on {self.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+        st = t.stride()
+        if st[2] != 1 or (heads > 1 and st[1] != self.dim):
+            raise ValueError(f"{what}: the heads of a token must be adjacent")
+        return t.data_ptr(), st[0] if n > 1 else heads * self.dim
+
+    def _place(self, page_table: torch.Tensor, lengths: torch.Tensor, offsets: Optional[torch.Tensor], n: int) -> Optional[int]:
+        """Sets the batch of a call; returns the address of the offsets."""
+        if lengths.dim() != 1 or page_table.dim() != 2:
+            raise ValueError("lengths is [B], page_table [B][max_pages]")
+        b = lengths.shape[0]
+        self.cfg.batch, self.cfg.max_pages = b, page_table.shape[1]
+        self.pages.lengths = self._need(lengths, torch.int32, (b,), "lengths")
+        self.pages.page_table = self._need(page_table, torch.int32, (b, page_table.shape[1]), "page_table")
+        if offsets is None:
+            if n != b:
+                raise ValueError(f"{n} tokens for {b} sequences: give the offsets")
+            return None
+        return self._need(offsets, torch.int32, (b + 1,), "offsets")
+
+    def _call(self, what: str, stream, call) -> None:
+        """call(stream) with the cache's device current."""
+        if self.device.type != "cuda":
+            raise ValueError(f"{what} runs on a GPU, the pages are on {self.device}")
+        st = binding._stream_of(stream, self.device)
+        if self.device.index is None or torch.cuda.current_device() == self.device.index:
+            rc = call(st)
+        else:
+            with torch.cuda.device(self.device):
+                rc = call(st)
+        if rc != 0:
+            raise PQCacheError(rc, what)
+
+    def _workspace(self, n: int, n_idx: int, stream):
+        size = self.lib.pqc_paged_workspace_bytes(self._cfg, n, n_idx)
+        ws = torch.empty(max(size, 256), dtype=torch.uint8, device=self.device)
+        if isinstance(stream, torch.cuda.Stream):
+            ws.record_stream(stream)  # not given to another tensor before the call has run there
+        return ws, ws.numel()
+
+    # -- entry points (same names as the C ABI)
+    def append(self, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor, *, new_offsets=None, q=None,
+               positions=None, q_out=None, k_out=None, stream=None):
+        """New tokens k, v [n][Hkv][D] (rows of a projection allowed) join their sequences; `lengths` counts them already.
+        With q [n][Hq][D] returns its rotated copy (q_out if given); k_out, if given, receives the rotated keys."""
+        n = k.shape[0]
+        off = self._place(page_table, lengths, new_offsets, n)
+        kp, ks = self._rows(k, n, self.heads, "k")
+        vp, vs = self._rows(v, n, self.heads, "v")
+        qp = qo = None
+        qs = 0
+        if q is not None:
+            qp, qs = self._rows(q, n, self.q_heads, "q")
+            if q_out is None:
+                q_out = torch.empty((n, self.q_heads, self.dim), dtype=self.io, device=self.device)
+            qo = self._need(q_out, self.io, (n, self.q_heads, self.dim), "q_out")
+        ko = None if k_out is None else self._need(k_out, self.io, (n, self.heads, self.dim), "k_out")
+        pos = None if positions is None else self._need(positions, torch.int32, (n,), "positions")
+        rot = None if self.rotation is None else self.rotation.data_ptr()
+        if n:
+            self._call("pqc_paged_append", stream,
+                       lambda st: self.lib.pqc_paged_append(self._cfg, self._pages, qp, qs, kp, ks, vp, vs, n, off, pos, rot, qo, ko, st))
+        return q_out
+
+    def attn(self, q: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor, *, q_offsets=None, out=None, stream=None):
+        """Attention of q [n][Hq][D] over all tokens of each sequence, causal; -> out [n][Hq][D]."""
+        n = q.shape[0]
+        off = self._place(page_table, lengths, q_offsets, n)
+        shape = (n, self.q_heads, self.dim)
+        qp = self._need(q, self.io, shape, "q")
+        if out is None:
+            out = torch.empty(shape, dtype=self.out, device=self.device)
+        op = self._need(out, self.out, shape, "out")
+        if n:
+            ws, size = self._workspace(n, 0, stream)
+            self._call("pqc_paged_attn", stream,
+                       lambda st: self.lib.pqc_paged_attn(self._cfg, self._pages, qp, n, off, op, ws.data_ptr(), size, st))
+        return out
+
+    def gather_attn(self, q: torch.Tensor, idx: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor, *, out=None, stream=None):
+        """Attention of q [B][Hq][D] over the tokens idx [B][Hkv][n_idx] int32 of each sequence; -> out [B][Hq][D]."""
+        b = q.shape[0]
+        self._place(page_table, lengths, None, b)
+        shape = (b, self.q_heads, self.dim)
+        qp = self._need(q, self.io, shape, "q")
+        if idx.dim() != 3 or idx.shape[2] < 1:
+            raise ValueError("idx is [B][Hkv][n_idx], n_idx >= 1")
+        ip = self._need(idx, torch.int32, (b, self.heads, idx.shape[2]), "idx")
+        if out is None:
+            out = torch.empty(shape, dtype=self.out, device=self.device)
+        op = self._need(out, self.out, shape, "out")
+        ws, size = self._workspace(b, idx.shape[2], stream)
+        self._call("pqc_paged_gather_attn", stream,
+                   lambda st: self.lib.pqc_paged_gather_attn(self._cfg, self._pages, qp, ip, idx.shape[2], op, ws.data_ptr(), size, st))
+        return out
