@@ -366,7 +366,8 @@ int pqc_block_cache_update(const pqc_config* cfg, int32_t block_tokens, int32_t 
  *
  *   k_pages, v_pages  [n_pages][Hkv][page_tokens][D]  cache_dtype
  *   k_scale, v_scale  [n_pages][Hkv] f32   PQC_FP8 only (else ignored, may be NULL): a row's
- *                                          values are code * scale of its page and head
+ *                                          values are code * scale of its page and head, a
+ *                                          power of two (as pqc_paged_append leaves it)
  *   page_table        [B][max_pages] int32 pages of sequence b; an entry outside
  *                                          [0, n_pages) is a page that is not there: nothing
  *                                          is written to it and none of its tokens attended
@@ -449,8 +450,8 @@ size_t pqc_paged_workspace_bytes(const pqc_paged_config* cfg, int32_t n, int32_t
  *   q    [n][Hq][D] io_dtype     out  [n][Hq][D] out_dtype
  *   workspace  256-byte aligned, pqc_paged_workspace_bytes(cfg, n, 0); contents need not be
  *              kept, calls that share it must be ordered on one stream
- * Sums, maxima and softmax weights are fp32; the weights enter the product with the values in
- * two bf16 terms for an fp32 output (2^-18 of a weight left out). */
+ * Sums, maxima and softmax weights are fp32; for a bf16 output the weights of calls with offsets may
+ * enter the product with the values rounded to bf16. */
 int pqc_paged_attn(const pqc_paged_config* cfg, const pqc_paged_cache* cache, const void* q, int32_t n,
                    const int32_t* offsets, void* out, void* workspace, size_t workspace_bytes, void* stream);
 

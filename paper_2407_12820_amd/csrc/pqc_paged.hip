@@ -15,6 +15,7 @@ bool aligned(const void* p, unsigned n) { return (reinterpret_cast<uintptr_t>(p)
 
 // Items per head that the length of a split aims at: about two workgroups of four waves per compute unit over all heads.
 constexpr int kItems = 512;
+constexpr int kBlockItems = 480;
 
 int make_geometry(const pqc_paged_config* c, long long n, Geometry* g) {
   if (!c) return PQC_EINVAL;
@@ -48,10 +49,17 @@ int make_geometry(const pqc_paged_config* c, long long n, Geometry* g) {
   return PQC_OK;
 }
 
-// Bounds of the items and of the partial results of a call with (at most) one or several query tokens per sequence.
-void plan_attn(Geometry* g, bool one_each) {
-  if (one_each) g->R = 1;
-  const int tiles = one_each ? g->B : (int)std::min<long long>(g->n_q, (long long)g->n_q / g->R + g->B);
+// What takes a call: a tile per query token, tiles of 16 rows, or (many queries per sequence) of 128 rows.
+enum class Tiles { kOne, kRows, kBlock };
+Tiles tiles_for(const pqc_paged_config* c, const Geometry& g, const int* offsets) {
+  if (!offsets) return Tiles::kOne;
+  return c->io_dtype == PQC_BF16 && (long long)g.n_q * g.G >= 32ll * g.B ? Tiles::kBlock : Tiles::kRows;
+}
+// Bounds of the items and of the partial results.
+void plan_attn(Geometry* g, Tiles form) {
+  g->R = form == Tiles::kOne ? 1 : (form == Tiles::kRows ? kRows : kBlockRows) / g->G;
+  if (form == Tiles::kBlock) g->per_head = std::max(1, (kBlockItems + g->Hkv - 1) / g->Hkv);
+  const int tiles = form == Tiles::kOne ? g->B : (int)std::min<long long>(g->n_q, (long long)g->n_q / g->R + g->B);
   g->items = tiles + g->per_head;
   g->slots = 2 * g->per_head;
 }
@@ -66,6 +74,14 @@ void plan_listed(Geometry* g, int n_idx) {
 }
 size_t partial_bytes(const Geometry& g, int head_dim) {
   return ((size_t)g.slots * g.Hkv * g.R * g.G * (head_dim + 2) * sizeof(float) + 255) / 256 * 256;
+}
+
+// Of whichever form takes a call.
+size_t attn_bytes(const pqc_paged_config* c, Geometry g) {
+  plan_attn(&g, Tiles::kRows);
+  const size_t rows = partial_bytes(g, c->head_dim);
+  plan_attn(&g, Tiles::kBlock);
+  return std::max(rows, partial_bytes(g, c->head_dim));
 }
 
 int check_cache(const pqc_paged_config* cfg, const pqc_paged_cache* c) {
@@ -103,6 +119,25 @@ void launch_rows(const AttnCall& a) {
     hipLaunchKernelGGL((attn_merge_kernel<D, LISTED>), dim3(split_tiles, g.Hkv, LISTED ? g.G : g.R * g.G), dim3(256), 0, a.st, g, a.c.lengths,
                        a.offsets, a.partials, a.out);
 }
+template <class C, int D>
+void launch_block(const AttnCall& a) {
+  const Geometry& g = a.g;
+  const dim3 grid((unsigned)(g.items * g.Hkv));
+  if (g.out_bf16)
+    hipLaunchKernelGGL((attn_block_kernel<C, D, 1>), grid, dim3(256), 0, a.st, g, a.c, static_cast<const bf16_t*>(a.q), a.offsets, a.out, a.partials);
+  else
+    hipLaunchKernelGGL((attn_block_kernel<C, D, 3>), grid, dim3(256), 0, a.st, g, a.c, static_cast<const bf16_t*>(a.q), a.offsets, a.out, a.partials);
+  if ((g.max_pages << g.shift) > kGrain)
+    hipLaunchKernelGGL((attn_merge_kernel<D, false>), dim3((unsigned)std::min(g.per_head, g.items - g.per_head), g.Hkv, kRows), dim3(256), 0, a.st, g,
+                       a.c.lengths, a.offsets, a.partials, a.out);
+}
+int launch_blocks(const pqc_paged_config* cfg, const AttnCall& a) {
+  if (cfg->cache_dtype == PQC_FP8)
+    cfg->head_dim == 128 ? launch_block<Fp8, 128>(a) : launch_block<Fp8, 64>(a);
+  else
+    cfg->head_dim == 128 ? launch_block<Bf16, 128>(a) : launch_block<Bf16, 64>(a);
+  return launched();
+}
 template <bool LISTED>
 int launch_attn(const pqc_paged_config* cfg, const AttnCall& a) {
   auto by_dim = [&](auto t, auto c) {
@@ -135,7 +170,7 @@ size_t pqc_paged_workspace_bytes(const pqc_paged_config* cfg, int32_t n, int32_t
   if (n_idx > 0)
     plan_listed(&g, n_idx);
   else
-    plan_attn(&g, false);
+    return attn_bytes(cfg, g);
   return partial_bytes(g, cfg->head_dim);
 }
 
@@ -147,13 +182,15 @@ int pqc_paged_attn(const pqc_paged_config* cfg, const pqc_paged_cache* cache, co
   rc = check_cache(cfg, cache);
   if (rc != PQC_OK) return rc;
   if (!q || !out || !aligned(q, 16) || !aligned(out, 16) || !aligned(offsets, 4) || (!offsets && n != g.B)) return PQC_EINVAL;
-  plan_attn(&g, false);
-  const size_t need = partial_bytes(g, cfg->head_dim);
-  if (!offsets) plan_attn(&g, true);
+  const size_t need = attn_bytes(cfg, g);
+  const Tiles form = tiles_for(cfg, g, offsets);
+  plan_attn(&g, form);
+  if ((long long)g.items * g.Hkv >= (1ll << 31)) return PQC_EUNSUPPORTED;
   if (!workspace || !aligned(workspace, 256) || workspace_bytes < need) return PQC_EWORKSPACE;
   if (n == 0) return PQC_OK;
   const Cache c = device_cache(cache);
-  return launch_attn<false>(cfg, AttnCall{g, c, q, offsets, nullptr, 0, out, static_cast<float*>(workspace), static_cast<hipStream_t>(stream)});
+  const AttnCall call{g, c, q, offsets, nullptr, 0, out, static_cast<float*>(workspace), static_cast<hipStream_t>(stream)};
+  return form == Tiles::kBlock ? launch_blocks(cfg, call) : launch_attn<false>(cfg, call);
 }
 
 int pqc_paged_gather_attn(const pqc_paged_config* cfg, const pqc_paged_cache* cache, const void* q, const int32_t* idx, int32_t n_idx, void* out,

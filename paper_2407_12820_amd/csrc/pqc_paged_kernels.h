@@ -11,6 +11,8 @@ namespace pqc {
 namespace paged {
 
 constexpr int kRows = 16;          // query rows of a tile: (query token, query head of the group) pairs
+constexpr int kBlockRows = 128;    // of a tile of the kernel for many queries
+constexpr int kBlockTokens = 64;   // tokens that it stages at a time
 constexpr int kStep = 32;          // tokens that a wave takes at a time
 constexpr int kWaves = 4;
 constexpr int kGrain = kWaves * kStep;  // tokens of a split are a multiple of this
@@ -103,9 +105,10 @@ __device__ __forceinline__ Item find_item(const Geometry& g, const int* lengths,
       const int at = j - before - (__builtin_amdgcn_readlane(end, l) - __builtin_amdgcn_readlane(count, l));
       it.b = b0 + l;
       it.n_split = __builtin_amdgcn_readlane(n, l);
-      it.tile = MERGE ? at : at / it.n_split;
-      it.split = MERGE ? 0 : at - it.tile * it.n_split;
-      it.slot = it.n_split > 1 ? slots + __builtin_amdgcn_readlane(slot_end - mine, l) + it.tile * it.n_split : -1;
+      const int nth = MERGE ? at : at / it.n_split;
+      it.tile = __builtin_amdgcn_readlane(tiles, l) - 1 - nth;  // the last one, which sees most, first
+      it.split = MERGE ? 0 : at - nth * it.n_split;
+      it.slot = it.n_split > 1 ? slots + __builtin_amdgcn_readlane(slot_end - mine, l) + nth * it.n_split : -1;
       it.s.first = __builtin_amdgcn_readlane(s.first, l);
       it.s.nq = __builtin_amdgcn_readlane(s.nq, l);
       it.s.len = __builtin_amdgcn_readlane(s.len, l);
@@ -149,8 +152,9 @@ struct Fp8 {
   template <int D> static constexpr int kLoads = D / 64;  // 16-byte loads of a key row per lane
   __device__ static __forceinline__ int dim(int f, int quad) { return 64 * (f >> 1) + 16 * quad + 8 * (f & 1); }
   __device__ static __forceinline__ int load_dim(int j, int quad) { return 64 * j + 16 * quad; }
-  static __device__ __forceinline__ unsigned two(unsigned x, bool high) {
-    const bf16x2_t p = high ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.0f, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.0f, false);
+  // two values times a power of two: the conversion adds exponents
+  static __device__ __forceinline__ unsigned two(unsigned x, bool high, float scale = 1.0f) {
+    const bf16x2_t p = high ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, false);
     unsigned u;
     __builtin_memcpy(&u, &p, 4);
     return u;
@@ -252,8 +256,10 @@ struct State {
 
 // One step: logits of 32 tokens, one rescaling if a maximum grew, weights, values.  `see(tile, i)` says whether the lane's query
 // sees its i-th token of the tile, `live(tile, i)` whether any query of the tile does (else its value row may hold anything, NaN
-// among it, and is taken as zero); both only matter if `masked` (wave-uniform).  The weights enter as two bf16 terms
-// (hi + lo, 2^-18 of the weight left out), because one would cost 2^-9 of the result.
+// among it, and is taken as zero); both only matter if `masked` (wave-uniform).  The weights enter as three bf16 terms,
+// whose sum is the fp32 weight: two leave out up to 2^-18 of it, which was the largest error of all over a few tokens (1.1e-6 of
+// the result against 1e-7), and the third is free where the bytes of the rows are what the step waits for.
+constexpr int kTerms = 3;
 template <typename T, class C, int D, class SeeFn, class LiveFn, class KsFn, class VsFn>
 __device__ __forceinline__ void attend(Stage<C, D>& st, const Query<T, C, D>& q, State<D>& a, bool masked, SeeFn see, LiveFn live, KsFn ks, VsFn vs) {
   float s[2][4];
@@ -292,7 +298,7 @@ __device__ __forceinline__ void attend(Stage<C, D>& st, const Query<T, C, D>& q,
 #pragma unroll
     for (int n = 0; n < D / 16; ++n) a.o[n] *= corr;
   }
-  u32x4_t hi, lo;
+  u32x4_t term[kTerms];
 #pragma unroll
   for (int tl = 0; tl < 2; ++tl)
 #pragma unroll
@@ -301,13 +307,17 @@ __device__ __forceinline__ void attend(Stage<C, D>& st, const Query<T, C, D>& q,
       a.l += p0 + p1;
       p0 *= vs(tl, i);
       p1 *= vs(tl, i + 1);
-      const unsigned h = pack_bf16(p0, p1);
-      hi[2 * tl + i / 2] = h;
-      lo[2 * tl + i / 2] = pack_bf16(p0 - __uint_as_float(h << 16), p1 - __uint_as_float(h & 0xffff0000u));
+#pragma unroll
+      for (int t = 0; t < kTerms; ++t) {
+        const unsigned h = pack_bf16(p0, p1);
+        term[t][2 * tl + i / 2] = h;
+        p0 -= __uint_as_float(h << 16);
+        p1 -= __uint_as_float(h & 0xffff0000u);
+      }
     }
-  bf16x8_t ph, pl;
-  __builtin_memcpy(&ph, &hi, 16);
-  __builtin_memcpy(&pl, &lo, 16);
+  bf16x8_t p[kTerms];
+#pragma unroll
+  for (int t = 0; t < kTerms; ++t) __builtin_memcpy(&p[t], &term[t], 16);
 #pragma unroll
   for (int j = 0; j < D / 32; ++j) {
     unsigned w[8];
@@ -322,10 +332,11 @@ __device__ __forceinline__ void attend(Stage<C, D>& st, const Query<T, C, D>& q,
     bf16x8_t v0, v1;
     __builtin_memcpy(&v0, &even, 16);
     __builtin_memcpy(&v1, &odd, 16);
-    a.o[2 * j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, ph, a.o[2 * j], 0, 0, 0);
-    a.o[2 * j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, ph, a.o[2 * j + 1], 0, 0, 0);
-    a.o[2 * j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, pl, a.o[2 * j], 0, 0, 0);
-    a.o[2 * j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, pl, a.o[2 * j + 1], 0, 0, 0);
+#pragma unroll
+    for (int t = 0; t < kTerms; ++t) {
+      a.o[2 * j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, p[t], a.o[2 * j], 0, 0, 0);
+      a.o[2 * j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, p[t], a.o[2 * j + 1], 0, 0, 0);
+    }
   }
 }
 
@@ -494,7 +505,7 @@ __global__ __launch_bounds__(256) void attn_merge_kernel(Geometry g, const int* 
                                                          const float* __restrict__ partials, void* __restrict__ out) {
   constexpr int kGroups = 256 / D;
   __shared__ float wave_m[4], red_o[kGroups][D], red_l[kGroups];
-  const int h = blockIdx.y, r = blockIdx.z;
+  const int h = blockIdx.y;
   Item it;
   if constexpr (LISTED) {
     it.b = blockIdx.x;
@@ -506,37 +517,311 @@ __global__ __launch_bounds__(256) void attn_merge_kernel(Geometry g, const int* 
     it = find_item<true>(g, lengths, offsets, blockIdx.x);
     if (it.b < 0) return;
   }
-  const int qr = it.tile * g.R + r / g.G;
-  if (qr >= it.s.nq) return;
   const int rows = g.R * g.G;
   const size_t stride = (size_t)g.Hkv * rows * (D + 2);
   const float* base = partials + ((size_t)it.slot * g.Hkv + h) * (size_t)(rows * (D + 2));
-  float m = kNegBig;
-  for (int i = threadIdx.x; i < it.n_split; i += 256) m = fmaxf(m, base[i * stride + rows * D + 2 * r]);
-  m = wave_max(m);
-  if ((threadIdx.x & 63) == 0) wave_m[threadIdx.x >> 6] = m;
-  __syncthreads();
-  m = fmaxf(fmaxf(wave_m[0], wave_m[1]), fmaxf(wave_m[2], wave_m[3]));
   const int d = threadIdx.x % D, part = threadIdx.x / D;
-  float o = 0.0f, l = 0.0f;
+  for (int r = blockIdx.z; r < rows; r += gridDim.z) {
+    const int qr = it.tile * g.R + r / g.G;
+    if (qr >= it.s.nq) return;
+    float m = kNegBig;
+    for (int i = threadIdx.x; i < it.n_split; i += 256) m = fmaxf(m, base[i * stride + rows * D + 2 * r]);
+    m = wave_max(m);
+    __syncthreads();  // the row before has been read
+    if ((threadIdx.x & 63) == 0) wave_m[threadIdx.x >> 6] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(wave_m[0], wave_m[1]), fmaxf(wave_m[2], wave_m[3]));
+    float o = 0.0f, l = 0.0f;
 #pragma unroll 4
-  for (int i = part; i < it.n_split; i += kGroups) {
-    const float* p = base + i * stride;
-    const float f = __builtin_amdgcn_exp2f(p[rows * D + 2 * r] - m);
-    l += f * p[rows * D + 2 * r + 1];
-    o += f * p[r * D + d];
-  }
-  red_o[part][d] = o;
-  if (d == 0) red_l[part] = l;
-  __syncthreads();
-  if (part == 0) {
-#pragma unroll
-    for (int i = 1; i < kGroups; ++i) {
-      o += red_o[i][d];
-      l += red_l[i];
+    for (int i = part; i < it.n_split; i += kGroups) {
+      const float* p = base + i * stride;
+      const float f = __builtin_amdgcn_exp2f(p[rows * D + 2 * r] - m);
+      l += f * p[rows * D + 2 * r + 1];
+      o += f * p[r * D + d];
     }
-    store_out(g, out, ((size_t)(it.s.first + qr) * g.Hq + (size_t)h * g.G + r % g.G) * D + d, l > 0.0f ? o / l : 0.0f);
+    red_o[part][d] = o;
+    if (d == 0) red_l[part] = l;
+    __syncthreads();
+    if (part == 0) {
+#pragma unroll
+      for (int i = 1; i < kGroups; ++i) {
+        o += red_o[i][d];
+        l += red_l[i];
+      }
+      store_out(g, out, ((size_t)(it.s.first + qr) * g.Hq + (size_t)h * g.G + r % g.G) * D + d, l > 0.0f ? o / l : 0.0f);
+    }
   }
+}
+
+// ------------------------------------------------------------------ many queries
+// Attention of tiles of 128 query rows: bound by the matrix cores and by the vector ALU's exponentials, not by bytes, so that
+// keys and values are brought into the form of the matrix instructions once per workgroup (LDS) and not once per 16 rows.
+// Four waves hold 32 rows each.  Per 64 tokens: S^T[64][32] = K Q^T and O^T[D][32] += V^T P^T, 32x32x16 instructions, whose first
+// operands are 16-byte LDS reads.  A wave's logits leave the first product in the lanes that need the weights as second operand
+// of the other one (lane col = query, half = l / 32: tokens 8 j + 4 half + 0..3), which the token order of V^T in LDS follows.
+//   K   [64 tokens][D]: 16-byte chunk c of token t lies at c ^ (t & 7)
+//   V^T [D][64 tokens]: chunk 2 k + half of dimension d, tokens 16 k + 4 half + {0..3, 8..11}, lies at c ^ (d ^ (d >> 2)) & 7
+// so that neither the staging stores nor the operands' reads meet in a bank.  The next 64 tokens' rows are loaded while these are
+// computed, the page of those behind them one round earlier.
+typedef __attribute__((ext_vector_type(16))) float f32x16_t;
+
+template <class C, int D>
+struct BlockStage {
+  static constexpr int kK = D / 64 * C::kBytes;           // 16-byte loads of keys per thread: token tid / 4
+  static constexpr int kV = C::kBytes;                    // words of each of eight tokens' values: four dimensions
+  static constexpr bool kHalfV = D == 64;                 // half of the threads stage values
+  u32x4_t k[kK];
+  unsigned v[8][kV];
+  float ks, vs;
+  bool k_ok, v_ok;
+  int token;  // the first of the 64
+
+  // pages of the thread's key token and of its eight value tokens
+  __device__ __forceinline__ void load(const Geometry& g, const Cache& c, int h, int t, int k_page, int v_page) {
+    const int tid = threadIdx.x;
+    token = t;
+    k_ok = k_page >= 0;
+    v_ok = v_page >= 0;
+    const size_t kp = (size_t)max(k_page, 0) * g.Hkv + h, vp = (size_t)max(v_page, 0) * g.Hkv + h;
+    ks = vs = 1.0f;
+    if constexpr (C::kBytes == 1) {
+      if (k_ok) ks = c.ks[kp];
+      if (v_ok) vs = c.vs[vp];
+    }
+    const unsigned char* kr = c.k + ((kp << g.shift) + ((t + tid / 4) & (g.P - 1))) * (size_t)(D * C::kBytes);
+    const int q = tid & 3;
+#pragma unroll
+    for (int j = 0; j < kK; ++j) {
+      const int dim = C::kBytes == 1 ? 64 * j + 16 * q : 64 * (j >> 1) + 16 * q + 8 * (j & 1);
+      k[j] = *reinterpret_cast<const u32x4_t*>(kr + dim * C::kBytes);
+    }
+    if (!kHalfV || tid < 128) {
+      const int chunk = tid / (D / 4), dg = tid % (D / 4);
+      const unsigned char* vr = c.v + ((vp << g.shift) + ((t + 16 * (chunk >> 1) + 4 * (chunk & 1)) & (g.P - 1))) * (size_t)(D * C::kBytes) + dg * 4 * C::kBytes;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) load_words(vr + (e < 4 ? e : e + 4) * (D * C::kBytes), v[e]);
+    }
+  }
+  // tokens from `most` on are zero, and those of pages that are not there
+  __device__ __forceinline__ void store(unsigned char* lk, unsigned char* lv, int most) {
+    const int tid = threadIdx.x, row = tid / 4, q = tid & 3;
+    if (!k_ok || token + row >= most) {
+#pragma unroll
+      for (int j = 0; j < kK; ++j) k[j] = u32x4_t{0u, 0u, 0u, 0u};
+      ks = 1.0f;
+    }
+    unsigned char* kr = lk + row * (D * 2);
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        u32x4_t w;
+        if constexpr (C::kBytes == 1)
+          w = u32x4_t{C::two(k[j][2 * e], false, ks), C::two(k[j][2 * e], true, ks), C::two(k[j][2 * e + 1], false, ks), C::two(k[j][2 * e + 1], true, ks)};
+        else
+          w = k[2 * j + e];
+        *reinterpret_cast<u32x4_t*>(kr + (((8 * j + 2 * q + e) ^ (row & 7)) << 4)) = w;
+      }
+    if (!kHalfV || tid < 128) {
+      const int chunk = tid / (D / 4), dg = tid % (D / 4);
+      const int first = token + 16 * (chunk >> 1) + 4 * (chunk & 1);
+      if (!v_ok || first + 12 > most) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (!v_ok || first + (e < 4 ? e : e + 4) >= most) {
+#pragma unroll
+            for (int i = 0; i < kV; ++i) v[e][i] = 0u;
+          }
+        if (!v_ok) vs = 1.0f;
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        u32x4_t even, odd;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          unsigned a, b;
+          if constexpr (C::kBytes == 1) {
+            a = C::two(v[2 * e][0], j == 1, vs);
+            b = C::two(v[2 * e + 1][0], j == 1, vs);
+          } else {
+            a = v[2 * e][j];
+            b = v[2 * e + 1][j];
+          }
+          even[e] = __builtin_amdgcn_perm(b, a, 0x05040100u);
+          odd[e] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+        }
+        const int d = 4 * dg + 2 * j;
+        *reinterpret_cast<u32x4_t*>(lv + d * 128 + ((chunk ^ ((d ^ (d >> 2)) & 7)) << 4)) = even;
+        *reinterpret_cast<u32x4_t*>(lv + (d + 1) * 128 + ((chunk ^ (((d + 1) ^ ((d + 1) >> 2)) & 7)) << 4)) = odd;
+      }
+    }
+  }
+};
+
+// TERMS: bf16 terms of a weight: one where the output is bf16 (2^-9 of a weight, no more than the output's own rounding), three
+// for an fp32 output.
+template <class C, int D, int TERMS>
+__global__ __launch_bounds__(256, 2) void attn_block_kernel(Geometry g, Cache c, const bf16_t* __restrict__ q, const int* __restrict__ offsets,
+                                                            void* __restrict__ out, float* __restrict__ partials) {
+  __shared__ __align__(16) unsigned char lds_k[2][kBlockTokens * D * 2], lds_v[2][kBlockTokens * D * 2];
+  __shared__ unsigned present[2];  // a byte per 16 tokens: their page is there
+  const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, half = lane >> 5, wave = tid >> 6;
+  // the heads of a KV head's tokens follow each other, so that with eight of them an XCD's L2 holds the rows of one
+  const int item = blockIdx.x / g.Hkv, h = blockIdx.x - item * g.Hkv;
+  const Item it = find_item<false>(g, c.lengths, offsets, item);
+  if (it.b < 0) return;
+  const int r = 32 * wave + col, qi = it.tile * g.R + r / g.G;
+  const bool row_ok = r < g.R * g.G && qi < it.s.nq;
+  const int hidden = it.s.len - it.s.nq;
+  const int lim = row_ok ? max(hidden + qi + 1, 0) : 0;
+  const int most = max(hidden + min((it.tile + 1) * g.R, it.s.nq), 0);
+  // what the wave's first and last rows see
+  const int row0 = 32 * wave, row1 = min(row0 + 31, g.R * g.G - 1);
+  const int least = row0 < g.R * g.G ? hidden + it.tile * g.R + row0 / g.G + 1 : 0;
+  const int wave_most = row0 < g.R * g.G ? min(most, hidden + it.tile * g.R + row1 / g.G + 1) : 0;
+  bf16x8_t qf[D / 16];
+  {
+    const bf16_t* row = q + ((size_t)(it.s.first + qi) * g.Hq + (size_t)h * g.G + r % g.G) * D + 8 * half;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+      u32x4_t x = {0u, 0u, 0u, 0u};
+      if (row_ok) x = *reinterpret_cast<const u32x4_t*>(row + 16 * i);
+      __builtin_memcpy(&qf[i], &x, 16);
+    }
+  }
+  f32x16_t o[D / 32];
+#pragma unroll
+  for (int n = 0; n < D / 32; ++n)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[n][i] = 0.0f;
+  float m = kNegBig, l = 0.0f;
+
+  const int t0 = it.split * it.tokens, t1 = it.n_split == 1 ? most : min(t0 + it.tokens, most);
+  if (t0 < t1) {
+    const int* table = c.table + (size_t)it.b * g.max_pages;
+    const int v_at = 16 * ((tid / (D / 4)) >> 1);  // the thread's value tokens' page (threads without any: some page of the row)
+    auto page_of = [&](int t) {
+      const int p = t < t1 ? table[t >> g.shift] : -1;
+      return p < g.n_pages ? p : -1;
+    };
+    BlockStage<C, D> st;
+    auto put = [&](int buf) {
+      st.store(lds_k[buf], lds_v[buf], most);
+      if ((tid & 63) == 0) reinterpret_cast<unsigned char*>(&present[buf])[wave] = (unsigned char)st.k_ok;  // wave: tokens 16 wave .. + 15
+    };
+    st.load(g, c, h, t0, page_of(t0 + tid / 4), page_of(t0 + (v_at & 63)));
+    int k_page = page_of(t0 + kBlockTokens + tid / 4), v_page = page_of(t0 + kBlockTokens + (v_at & 63));
+    put(0);
+    __syncthreads();
+    for (int t = t0, buf = 0; t < t1; t += kBlockTokens, buf ^= 1) {
+      const bool more = t + kBlockTokens < t1;
+      if (more) {
+        st.load(g, c, h, t + kBlockTokens, k_page, v_page);
+        k_page = page_of(t + 2 * kBlockTokens + tid / 4);
+        v_page = page_of(t + 2 * kBlockTokens + (v_at & 63));
+      }
+      if (t < wave_most) {
+        f32x16_t s[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[b][i] = 0.0f;
+          const int row = 32 * b + col;
+#pragma unroll
+          for (int i = 0; i < D / 16; ++i) {
+            bf16x8_t k;
+            __builtin_memcpy(&k, lds_k[buf] + row * (D * 2) + (((2 * i + half) ^ (row & 7)) << 4), 16);
+            s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, qf[i], s[b], 0, 0, 0);
+          }
+        }
+        const unsigned there = __builtin_amdgcn_readfirstlane(present[buf]);
+        if (t + kBlockTokens > least || there != 0x01010101u) {
+#pragma unroll
+          for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const int at = 32 * b + 8 * (i >> 2) + 4 * half + (i & 3);
+              if (t + at >= lim || !((there >> (8 * (at >> 4))) & 1u)) s[b][i] = -INFINITY;
+            }
+        }
+        float mx = kNegBig;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, fmaxf(s[0][i], s[1][i]));
+        const u32x2_t both = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+        mx = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * g.scale_log2e;
+        // weights may reach 2^8 before a larger maximum is taken: they are relative to it in O and l alike
+        if (__any(mx > m + 8.0f)) {
+          const float mnew = fmaxf(m, mx), corr = __builtin_amdgcn_exp2f(m - mnew);
+          m = mnew;
+          l *= corr;
+#pragma unroll
+          for (int n = 0; n < D / 32; ++n) o[n] *= corr;
+        }
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          unsigned w[TERMS][8];
+#pragma unroll
+          for (int i = 0; i < 16; i += 2) {
+            float p0 = __builtin_amdgcn_exp2f(fmaf(s[b][i], g.scale_log2e, -m)), p1 = __builtin_amdgcn_exp2f(fmaf(s[b][i + 1], g.scale_log2e, -m));
+            l += p0 + p1;
+#pragma unroll
+            for (int e = 0; e < TERMS; ++e) {
+              w[e][i / 2] = pack_bf16(p0, p1);
+              p0 -= __uint_as_float(w[e][i / 2] << 16);
+              p1 -= __uint_as_float(w[e][i / 2] & 0xffff0000u);
+            }
+          }
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            bf16x8_t p[TERMS];
+#pragma unroll
+            for (int e = 0; e < TERMS; ++e) __builtin_memcpy(&p[e], &w[e][4 * k], 16);
+#pragma unroll
+            for (int n = 0; n < D / 32; ++n) {
+              const int d = 32 * n + col;
+              bf16x8_t v;
+              __builtin_memcpy(&v, lds_v[buf] + d * 128 + (((2 * (2 * b + k) + half) ^ ((d ^ (d >> 2)) & 7)) << 4), 16);
+#pragma unroll
+              for (int e = 0; e < TERMS; ++e) o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[e], o[n], 0, 0, 0);
+            }
+          }
+        }
+      }
+      if (more) put(buf ^ 1);
+      __syncthreads();
+    }
+  }
+  const u32x2_t both = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+  l = __uint_as_float(both[0]) + __uint_as_float(both[1]);
+  if (r >= g.R * g.G) return;
+  if (it.slot >= 0) {
+    const int rows = g.R * g.G;
+    float* po = partials + ((size_t)(it.slot + it.split) * g.Hkv + h) * (size_t)(rows * (D + 2));
+#pragma unroll
+    for (int n = 0; n < D / 32; ++n)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) po[r * D + 32 * n + 8 * j + 4 * half + i] = o[n][4 * j + i];
+    if (half == 0) {
+      po[rows * D + 2 * r] = m;
+      po[rows * D + 2 * r + 1] = l;
+    }
+    return;
+  }
+  if (!row_ok) return;
+  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+  const size_t at = ((size_t)(it.s.first + qi) * g.Hq + (size_t)h * g.G + r % g.G) * D + 4 * half;
+#pragma unroll
+  for (int n = 0; n < D / 32; ++n)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const size_t a = at + 32 * n + 8 * j;
+      if (g.out_bf16)
+        *reinterpret_cast<u32x2_t*>(static_cast<bf16_t*>(out) + a) = u32x2_t{pack_bf16(o[n][4 * j] * inv, o[n][4 * j + 1] * inv), pack_bf16(o[n][4 * j + 2] * inv, o[n][4 * j + 3] * inv)};
+      else
+        *reinterpret_cast<f32x4_t*>(static_cast<float*>(out) + a) = f32x4_t{o[n][4 * j] * inv, o[n][4 * j + 1] * inv, o[n][4 * j + 2] * inv, o[n][4 * j + 3] * inv};
+    }
 }
 
 // ------------------------------------------------------------------ append

@@ -7,7 +7,7 @@ allocated per call from torch's caching allocator, hence two streams, or two cap
 from __future__ import annotations
 
 import ctypes as C
-from typing import Optional, Tuple
+from typing import Optional
 
 import torch
 
@@ -55,6 +55,8 @@ def rotation_table(n_positions: int, rot_dims: int, base: float = 10000.0, devic
     return torch.cat([angle.cos(), angle.sin()], 1).to(torch.float32).contiguous()
 
 
+# The small calls are shorter than what Python does in front of them, so that each tensor is checked in one expression on the
+# quickest of torch's accessors, and what is wrong is worked out by _need and _rows only if something is.
 class PagedCache:
     """Pages [n_pages][Hkv][page_tokens][D] of keys and of values, float8_e4m3fn with scales [n_pages][Hkv] f32, or bfloat16
     (scales None).  Like a decode context it is not thread-safe.  `dtype`: "f32" or "bf16", of q, k and v; `out_dtype`: of the attention output; `rotation`: the table of
@@ -81,12 +83,15 @@ class PagedCache:
         if rotation is not None:
             rot_positions, rot_dims = rotation.shape
             self._need(rotation, torch.float32, rotation.shape, "rotation")
+        self._rotation = None if rotation is None else rotation.data_ptr()
         self.heads, self.dim, self.q_heads = heads, dim, n_q_heads
         self.cfg = Config(1, n_q_heads, heads, dim, tokens, n_pages, 1, _DTYPES[dtype][0], 2 if fp8 else 1, _DTYPES[out_dtype][0],
                           softmax_scale, rot_dims, _STYLES[rot_style], rot_positions)
         self.pages = Pages(k_pages.data_ptr(), v_pages.data_ptr(), k_scale.data_ptr() if fp8 else None,
                            v_scale.data_ptr() if fp8 else None, None, None)
         self._cfg, self._pages = C.byref(self.cfg), C.byref(self.pages)
+        self._dev = k_pages.get_device()
+        self._sizes = {}  # workspace bytes by (batch, listed tokens)
 
     @classmethod
     def empty(cls, n_pages: int, n_q_heads: int, n_kv_heads: int, head_dim: int = 128, page_tokens: int = 64, cache_dtype: str = "fp8",
@@ -106,101 +111,115 @@ class PagedCache:
             raise ValueError(f"{what}: expected contiguous {dtype} {tuple(shape)} on {self.device}, got {got}")
         return t.data_ptr()
 
-    def _rows(self, t: torch.Tensor, n: int, heads: int, what: str) -> Tuple[int, int]:
-        """Address and token stride of [n][heads][D] whose heads are adjacent."""
-        if t.dtype is not self.io or t.shape != (n, heads, self.dim) or t.device != self.device:
+    def _rows(self, t: torch.Tensor, n: int, heads: int, what: str) -> int:
+        """Token stride of [n][heads][D] whose heads are adjacent."""
+        if t.dtype is not self.io or t.shape != (n, heads, self.dim) or t.get_device() != self._dev:
             raise ValueError(f"{what}: expected {self.io} {(n, heads, self.dim)} on {self.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
-        st = t.stride()
-        if st[2] != 1 or (heads > 1 and st[1] != self.dim):
+        token, head, one = t.stride()
+        if one != 1 or (head != self.dim and heads > 1):
             raise ValueError(f"{what}: the heads of a token must be adjacent")
-        return t.data_ptr(), st[0] if n > 1 else heads * self.dim
+        return token if n > 1 else heads * self.dim
 
     def _place(self, page_table: torch.Tensor, lengths: torch.Tensor, offsets: Optional[torch.Tensor], n: int) -> Optional[int]:
         """Sets the batch of a call; returns the address of the offsets."""
-        if lengths.dim() != 1 or page_table.dim() != 2:
-            raise ValueError("lengths is [B], page_table [B][max_pages]")
-        b = lengths.shape[0]
-        self.cfg.batch, self.cfg.max_pages = b, page_table.shape[1]
-        self.pages.lengths = self._need(lengths, torch.int32, (b,), "lengths")
-        self.pages.page_table = self._need(page_table, torch.int32, (b, page_table.shape[1]), "page_table")
-        if offsets is None:
-            if n != b:
-                raise ValueError(f"{n} tokens for {b} sequences: give the offsets")
-            return None
-        return self._need(offsets, torch.int32, (b + 1,), "offsets")
+        shape = page_table.shape
+        if len(shape) != 2:
+            raise ValueError("page_table is [B][max_pages]")
+        b, most = shape
+        if lengths.dtype is not torch.int32 or lengths.shape != (b,) or not lengths.is_contiguous() or lengths.get_device() != self._dev:
+            self._need(lengths, torch.int32, (b,), "lengths")
+        if page_table.dtype is not torch.int32 or not page_table.is_contiguous() or page_table.get_device() != self._dev:
+            self._need(page_table, torch.int32, shape, "page_table")
+        cfg, pages = self.cfg, self.pages
+        cfg.batch, cfg.max_pages = b, most
+        pages.page_table, pages.lengths = page_table.data_ptr(), lengths.data_ptr()
+        if offsets is not None:
+            return self._need(offsets, torch.int32, (b + 1,), "offsets")
+        if n != b:
+            raise ValueError(f"{n} tokens for {b} sequences: give the offsets")
+        return None
 
-    def _call(self, what: str, stream, call) -> None:
-        """call(stream) with the cache's device current."""
-        if self.device.type != "cuda":
+    def _plain(self, t: torch.Tensor, dtype, n: int, heads: int, what: str) -> int:
+        """Address of a contiguous [n][heads][D]."""
+        if t.dtype is not dtype or t.shape != (n, heads, self.dim) or not t.is_contiguous() or t.get_device() != self._dev:
+            self._need(t, dtype, (n, heads, self.dim), what)
+        return t.data_ptr()
+
+    def _call(self, what: str, fn, stream, args) -> None:
+        """fn(*args, stream) with the cache's device current."""
+        if self._dev < 0:
             raise ValueError(f"{what} runs on a GPU, the pages are on {self.device}")
-        st = binding._stream_of(stream, self.device)
-        if self.device.index is None or torch.cuda.current_device() == self.device.index:
-            rc = call(st)
+        st = torch._C._cuda_getCurrentRawStream(self._dev) if stream is None else stream.cuda_stream
+        if torch._C._cuda_getDevice() == self._dev:
+            rc = fn(*args, st)
         else:
-            with torch.cuda.device(self.device):
-                rc = call(st)
+            with torch.cuda.device(self._dev):
+                rc = fn(*args, st)
         if rc != 0:
             raise PQCacheError(rc, what)
 
-    def _workspace(self, n: int, n_idx: int, stream):
-        size = self.lib.pqc_paged_workspace_bytes(self._cfg, n, n_idx)
-        ws = torch.empty(max(size, 256), dtype=torch.uint8, device=self.device)
-        if isinstance(stream, torch.cuda.Stream):
+    def _workspace(self, batch: int, n_idx: int, stream):
+        size = self._sizes.get((batch, n_idx))
+        if size is None:
+            if len(self._sizes) >= 256:
+                self._sizes.clear()
+            size = self._sizes[batch, n_idx] = self.lib.pqc_paged_workspace_bytes(self._cfg, batch, n_idx)
+        if not size:
+            return None, None
+        ws = torch.empty(size, dtype=torch.uint8, device=self.device)
+        if stream is not None and self._dev >= 0:
             ws.record_stream(stream)  # not given to another tensor before the call has run there
-        return ws, ws.numel()
+        return ws, ws.data_ptr()
 
     # -- entry points (same names as the C ABI)
     def append(self, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor, *, new_offsets=None, q=None,
                positions=None, q_out=None, k_out=None, stream=None):
         """New tokens k, v [n][Hkv][D] (rows of a projection allowed) join their sequences; `lengths` counts them already.
         With q [n][Hq][D] returns its rotated copy (q_out if given); k_out, if given, receives the rotated keys."""
-        n = k.shape[0]
+        n, heads = k.shape[0], self.heads
         off = self._place(page_table, lengths, new_offsets, n)
-        kp, ks = self._rows(k, n, self.heads, "k")
-        vp, vs = self._rows(v, n, self.heads, "v")
-        qp = qo = None
-        qs = 0
+        k_stride, v_stride = self._rows(k, n, heads, "k"), self._rows(v, n, heads, "v")
+        qp = qo = ko = pos = None
+        q_stride = 0
         if q is not None:
-            qp, qs = self._rows(q, n, self.q_heads, "q")
+            q_stride, qp = self._rows(q, n, self.q_heads, "q"), q.data_ptr()
             if q_out is None:
                 q_out = torch.empty((n, self.q_heads, self.dim), dtype=self.io, device=self.device)
-            qo = self._need(q_out, self.io, (n, self.q_heads, self.dim), "q_out")
-        ko = None if k_out is None else self._need(k_out, self.io, (n, self.heads, self.dim), "k_out")
-        pos = None if positions is None else self._need(positions, torch.int32, (n,), "positions")
-        rot = None if self.rotation is None else self.rotation.data_ptr()
+            qo = self._plain(q_out, self.io, n, self.q_heads, "q_out")
+        if k_out is not None:
+            ko = self._plain(k_out, self.io, n, heads, "k_out")
+        if positions is not None:
+            pos = self._need(positions, torch.int32, (n,), "positions")
         if n:
-            self._call("pqc_paged_append", stream,
-                       lambda st: self.lib.pqc_paged_append(self._cfg, self._pages, qp, qs, kp, ks, vp, vs, n, off, pos, rot, qo, ko, st))
+            self._call("pqc_paged_append", self.lib.pqc_paged_append, stream,
+                       (self._cfg, self._pages, qp, q_stride, k.data_ptr(), k_stride, v.data_ptr(), v_stride, n, off, pos, self._rotation, qo, ko))
         return q_out
 
     def attn(self, q: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor, *, q_offsets=None, out=None, stream=None):
         """Attention of q [n][Hq][D] over all tokens of each sequence, causal; -> out [n][Hq][D]."""
         n = q.shape[0]
         off = self._place(page_table, lengths, q_offsets, n)
-        shape = (n, self.q_heads, self.dim)
-        qp = self._need(q, self.io, shape, "q")
+        qp = self._plain(q, self.io, n, self.q_heads, "q")
         if out is None:
-            out = torch.empty(shape, dtype=self.out, device=self.device)
-        op = self._need(out, self.out, shape, "out")
+            out = torch.empty((n, self.q_heads, self.dim), dtype=self.out, device=self.device)
+        op = self._plain(out, self.out, n, self.q_heads, "out")
         if n:
-            ws, size = self._workspace(n, 0, stream)
-            self._call("pqc_paged_attn", stream,
-                       lambda st: self.lib.pqc_paged_attn(self._cfg, self._pages, qp, n, off, op, ws.data_ptr(), size, st))
+            ws, wp = self._workspace(self.cfg.batch, 0, stream)
+            self._call("pqc_paged_attn", self.lib.pqc_paged_attn, stream, (self._cfg, self._pages, qp, n, off, op, wp, 0 if ws is None else ws.numel()))
         return out
 
     def gather_attn(self, q: torch.Tensor, idx: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor, *, out=None, stream=None):
         """Attention of q [B][Hq][D] over the tokens idx [B][Hkv][n_idx] int32 of each sequence; -> out [B][Hq][D]."""
         b = q.shape[0]
         self._place(page_table, lengths, None, b)
-        shape = (b, self.q_heads, self.dim)
-        qp = self._need(q, self.io, shape, "q")
-        if idx.dim() != 3 or idx.shape[2] < 1:
-            raise ValueError("idx is [B][Hkv][n_idx], n_idx >= 1")
-        ip = self._need(idx, torch.int32, (b, self.heads, idx.shape[2]), "idx")
+        qp = self._plain(q, self.io, b, self.q_heads, "q")
+        n_idx = idx.shape[-1]
+        if n_idx < 1 or idx.dtype is not torch.int32 or idx.shape != (b, self.heads, n_idx) or not idx.is_contiguous() or idx.get_device() != self._dev:
+            self._need(idx, torch.int32, (b, self.heads, max(n_idx, 1)), "idx")
         if out is None:
-            out = torch.empty(shape, dtype=self.out, device=self.device)
-        op = self._need(out, self.out, shape, "out")
-        ws, size = self._workspace(b, idx.shape[2], stream)
-        self._call("pqc_paged_gather_attn", stream,
-                   lambda st: self.lib.pqc_paged_gather_attn(self._cfg, self._pages, qp, ip, idx.shape[2], op, ws.data_ptr(), size, st))
+            out = torch.empty((b, self.q_heads, self.dim), dtype=self.out, device=self.device)
+        op = self._plain(out, self.out, b, self.q_heads, "out")
+        ws, wp = self._workspace(b, n_idx, stream)
+        self._call("pqc_paged_gather_attn", self.lib.pqc_paged_gather_attn, stream,
+                   (self._cfg, self._pages, qp, idx.data_ptr(), n_idx, op, wp, 0 if ws is None else ws.numel()))
         return out
