@@ -13,8 +13,13 @@ using namespace pqc::paged;
 
 bool aligned(const void* p, unsigned n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
-// Items per head that the length of a split aims at: about two workgroups of four waves per compute unit over all heads.
-constexpr int kItems = 512;
+// Workgroups of the kernel of 16 rows over all heads: two per compute unit.  One per compute unit leaves its start and its tiles' ends
+// uncovered (48 ragged sequences, 8 heads of 8 query heads, 280 MB: 80.5 us, two 70.4, three 79.9; a single sequence of 131072 tokens 64.9, 59.0,
+// 66.9).  kRowsLds, beyond the kernel's own arrays, keeps a third off a compute unit: with room for three the 512 are spread unevenly (8
+// sequences of 68224 tokens 233 us, 202 with it).
+constexpr int kWorkers = 512;
+constexpr size_t kRowsLds = 56 * 1024;
+// Items of the kernel of 128 rows that the length of a split aims at.
 constexpr int kBlockItems = 480;
 
 int make_geometry(const pqc_paged_config* c, long long n, Geometry* g) {
@@ -44,8 +49,7 @@ int make_geometry(const pqc_paged_config* c, long long n, Geometry* g) {
   g->out_bf16 = c->out_dtype == PQC_BF16;
   const float scale = c->softmax_scale > 0.0f ? c->softmax_scale : 1.0f / std::sqrt((float)c->head_dim);
   g->scale_log2e = scale * 1.4426950408889634f;
-  g->per_head = std::max(1, (kItems + g->Hkv - 1) / g->Hkv);
-  g->items = g->slots = g->split = g->n_split = 0;
+  g->per_head = g->items = g->slots = g->workers = g->grain = 0;
   return PQC_OK;
 }
 
@@ -55,25 +59,30 @@ Tiles tiles_for(const pqc_paged_config* c, const Geometry& g, const int* offsets
   if (!offsets) return Tiles::kOne;
   return c->io_dtype == PQC_BF16 && (long long)g.n_q * g.G >= 32ll * g.B ? Tiles::kBlock : Tiles::kRows;
 }
-// Bounds of the items and of the partial results.
+// The kernel of 16 rows: workers, and units small enough for 32 bits over `tiles` tiles of at most `tokens` tokens.
+void plan_rows(Geometry* g, long long tiles, long long tokens) {
+  g->workers = std::max(1, kWorkers / g->Hkv);
+  g->grain = kGrain;
+  while (tiles * (tokens / g->grain + 1 + kTileCost) >= (1ll << 30) - g->workers) g->grain *= 2;
+  g->slots = tokens > g->grain ? 2 * g->workers : 0;  // else no border lies inside a tile
+}
 void plan_attn(Geometry* g, Tiles form) {
   g->R = form == Tiles::kOne ? 1 : (form == Tiles::kRows ? kRows : kBlockRows) / g->G;
-  if (form == Tiles::kBlock) g->per_head = std::max(1, (kBlockItems + g->Hkv - 1) / g->Hkv);
-  const int tiles = form == Tiles::kOne ? g->B : (int)std::min<long long>(g->n_q, (long long)g->n_q / g->R + g->B);
-  g->items = tiles + g->per_head;
+  const long long tiles = form == Tiles::kOne ? g->B : std::min<long long>(g->n_q, (long long)g->n_q / g->R + g->B);
+  if (form != Tiles::kBlock) {
+    plan_rows(g, tiles, (long long)g->max_pages << g->shift);
+    return;
+  }
+  g->per_head = std::max(1, (kBlockItems + g->Hkv - 1) / g->Hkv);
+  g->items = (int)tiles + g->per_head;
   g->slots = 2 * g->per_head;
 }
-// Listed tokens: the splits of a sequence are as many as give the items of all sequences the number aimed at.
 void plan_listed(Geometry* g, int n_idx) {
   g->R = 1;
-  const long long most = std::max(1, g->per_head / g->B);
-  g->split = (int)(((n_idx + most - 1) / most + kGrain - 1) / kGrain) * kGrain;
-  g->split = std::max(g->split, kGrain);
-  g->n_split = std::max(1, (n_idx + g->split - 1) / g->split);
-  g->slots = g->n_split > 1 ? g->B * g->n_split : 0;
+  plan_rows(g, g->B, n_idx);
 }
 size_t partial_bytes(const Geometry& g, int head_dim) {
-  return ((size_t)g.slots * g.Hkv * g.R * g.G * (head_dim + 2) * sizeof(float) + 255) / 256 * 256;
+  return ((size_t)g.slots * g.Hkv * partial_floats(g.R * g.G, head_dim) * sizeof(float) + 255) / 256 * 256;
 }
 
 // Of whichever form takes a call.
@@ -110,14 +119,12 @@ struct AttnCall {
 template <typename T, class C, int D, bool LISTED>
 void launch_rows(const AttnCall& a) {
   const Geometry& g = a.g;
-  const unsigned items = LISTED ? (unsigned)(g.B * g.n_split) : (unsigned)g.items;
-  hipLaunchKernelGGL((attn_rows_kernel<T, C, D, LISTED>), dim3(items, g.Hkv), dim3(256), 0, a.st, g, a.c, static_cast<const T*>(a.q), a.offsets, a.idx,
-                     a.n_idx, a.out, a.partials);
-  // tiles of several splits have two items at least
-  const unsigned split_tiles = LISTED ? (unsigned)g.B : (unsigned)std::min(g.per_head, g.items - g.per_head);
-  if (LISTED ? g.n_split > 1 : (g.max_pages << g.shift) > kGrain)
-    hipLaunchKernelGGL((attn_merge_kernel<D, LISTED>), dim3(split_tiles, g.Hkv, LISTED ? g.G : g.R * g.G), dim3(256), 0, a.st, g, a.c.lengths,
-                       a.offsets, a.partials, a.out);
+  constexpr size_t lds = kRowsLds - rows_static_lds(D);
+  hipLaunchKernelGGL((attn_rows_kernel<T, C, D, LISTED>), dim3((unsigned)(g.workers * g.Hkv)), dim3(256), lds, a.st, g, a.c,
+                     static_cast<const T*>(a.q), a.offsets, a.idx, a.n_idx, a.out, a.partials);
+  if (g.workers > 1 && g.slots > 0)
+    hipLaunchKernelGGL((attn_merge_kernel<D, true, 8>), dim3((unsigned)g.workers - 1, g.Hkv, g.R * g.G), dim3(256), 0, a.st, g, a.c.lengths, a.offsets,
+                       LISTED ? a.n_idx : -1, a.partials, a.out);
 }
 template <class C, int D>
 void launch_block(const AttnCall& a) {
@@ -128,8 +135,8 @@ void launch_block(const AttnCall& a) {
   else
     hipLaunchKernelGGL((attn_block_kernel<C, D, 3>), grid, dim3(256), 0, a.st, g, a.c, static_cast<const bf16_t*>(a.q), a.offsets, a.out, a.partials);
   if ((g.max_pages << g.shift) > kGrain)
-    hipLaunchKernelGGL((attn_merge_kernel<D, false>), dim3((unsigned)std::min(g.per_head, g.items - g.per_head), g.Hkv, kRows), dim3(256), 0, a.st, g,
-                       a.c.lengths, a.offsets, a.partials, a.out);
+    hipLaunchKernelGGL((attn_merge_kernel<D, false, 1>), dim3((unsigned)std::min(g.per_head, g.items - g.per_head), g.Hkv, 4), dim3(256), 0, a.st, g,
+                       a.c.lengths, a.offsets, -1, a.partials, a.out);
 }
 int launch_blocks(const pqc_paged_config* cfg, const AttnCall& a) {
   if (cfg->cache_dtype == PQC_FP8)
@@ -234,7 +241,9 @@ int pqc_paged_append(const pqc_paged_config* cfg, const pqc_paged_cache* cache, 
   a.rot = cfg->rot_dims; a.rot_positions = cfg->rot_positions;
   a.pairs = cfg->rot_style == PQC_ROT_PAIRS;
   a.q_out = q_out; a.k_out = k_out;
-  a.q_tokens = n > 4096 ? 4 : 1;
+  // query tokens per workgroup: up to 32, as long as there are several workgroups per compute unit
+  a.q_tokens = 1;
+  while (a.q_tokens < 32 && n >= 1024 * a.q_tokens) a.q_tokens *= 2;
   // a sequence of m tokens touches at most 1 + (m + P - 2) / P pages, and no more than m
   const long long pages = offsets ? std::min<long long>(n, (long long)n / g.P + 2ll * g.B) : n;
   if (pages * 2 * g.Hkv + n >= (1ll << 31)) return PQC_EUNSUPPORTED;

@@ -30,7 +30,7 @@ struct Geometry {
   int R;                  // query tokens per tile
   int per_head;           // items per head that the split length aims at
   int items, slots;       // bounds of the numbers of items and of partial results per head
-  int split, n_split;     // listed tokens: tokens per split and splits (the same for every head)
+  int workers, grain;     // kernel of 16 rows: workgroups per head, tokens of a unit of their work
   bool out_bf16;
   float scale_log2e;
 };
@@ -39,6 +39,9 @@ struct Cache {
   float *ks, *vs;
   const int *table, *lengths;
 };
+
+// A partial result: O[rows][D], then maximum and sum of every row; 16-byte aligned.
+__host__ __device__ constexpr size_t partial_floats(int rows, int dim) { return (size_t)rows * dim + (2 * rows + 3) / 4 * 4; }
 
 // ------------------------------------------------------------------ sequences and items
 struct Seq {
@@ -118,6 +121,85 @@ __device__ __forceinline__ Item find_item(const Geometry& g, const int* lengths,
     slots += wave_last(slot_end);
   }
   return it;
+}
+
+// The kernel of 16 rows, which waits for bytes: all tiles of a head laid end to end, one per query tile of every sequence, a tile
+// being its sequence's tokens in units of `grain` and kTileCost units in front of them for what a tile costs by itself.  Every
+// worker of the head takes the same share of units, wherever that begins and ends, so that the workgroups, which are all
+// resident at once, end together: 48 ragged sequences of 8 heads as whole splits over 512 workgroups took 80 us.  A border inside a
+// tile's first kTileCost units counts as its beginning.
+constexpr int kTileCost = 2;
+struct Border {
+  int b, tile, unit;  // unit 0: the tile's beginning
+  int tiles, units;   // of the sequence, of each of its tiles
+  int at;             // of the border's tile in the sum of all units
+  Seq s;
+};
+// listed >= 0: every sequence has one tile of that many tokens.
+__device__ __forceinline__ int tile_units(const Geometry& g, const Seq& s, int listed, int& tiles) {
+  tiles = listed >= 0 ? 1 : (s.nq + g.R - 1) / g.R;
+  return max(1, ((listed >= 0 ? listed : s.len) + g.grain - 1) / g.grain) + kTileCost;
+}
+// Units of a share, and the border at `nth` shares (b = B: there is none).  Up to 64 sequences take one load, one lane each.
+__device__ __forceinline__ Border border_of(const Geometry& g, const int* lengths, const int* offsets, int listed, int nth, int& total, int& share) {
+  Border r;
+  r.b = g.B;
+  if (listed >= 0) {
+    r.s = Seq{0, 1, 0};
+    r.units = tile_units(g, r.s, listed, r.tiles);
+    total = r.units * g.B;
+    share = (total + g.workers - 1) / g.workers;
+    const int x = nth * share;
+    if (x >= total) return r;
+    r.b = r.s.first = x / r.units;
+    r.s.len = seq_of(g, lengths, nullptr, r.b).len;
+    r.tile = 0;
+    r.at = r.b * r.units;
+    r.unit = max(x - r.at - kTileCost, 0);
+    return r;
+  }
+  const int lane = threadIdx.x & 63;
+  Seq s{0, 0, 0};
+  int tiles = 0, units = 1, end = 0;
+  auto look = [&](int b0) {
+    s = Seq{0, 0, 0};
+    tiles = 0;
+    units = 1;
+    if (b0 + lane < g.B) {
+      s = seq_of(g, lengths, offsets, b0 + lane);
+      units = tile_units(g, s, listed, tiles);
+    }
+    end = wave_inclusive_scan(tiles * units);
+  };
+  total = 0;
+  for (int b0 = 0; b0 < g.B; b0 += 64) {
+    look(b0);
+    total += wave_last(end);
+  }
+  share = (total + g.workers - 1) / g.workers;
+  const int x = nth * share;
+  if (x >= total) return r;
+  int before = 0;
+  for (int b0 = 0; b0 < g.B; b0 += 64) {
+    if (g.B > 64) look(b0);
+    const unsigned long long has = __ballot(before + end > x);
+    if (has) {
+      const int l = __ffsll((long long)has) - 1;
+      r.b = b0 + l;
+      r.tiles = __builtin_amdgcn_readlane(tiles, l);
+      r.units = __builtin_amdgcn_readlane(units, l);
+      const int first = before + __builtin_amdgcn_readlane(end, l) - r.tiles * r.units;
+      r.tile = (x - first) / r.units;
+      r.at = first + r.tile * r.units;
+      r.unit = max(x - r.at - kTileCost, 0);
+      r.s.first = __builtin_amdgcn_readlane(s.first, l);
+      r.s.nq = __builtin_amdgcn_readlane(s.nq, l);
+      r.s.len = __builtin_amdgcn_readlane(s.len, l);
+      return r;
+    }
+    before += wave_last(end);
+  }
+  return r;
 }
 
 // Maximum and sum over the four lanes l, l^16, l^32, l^48.
@@ -260,8 +342,10 @@ struct State {
 // whose sum is the fp32 weight: two leave out up to 2^-18 of it, which was the largest error of all over a few tokens (1.1e-6 of
 // the result against 1e-7), and the third is free where the bytes of the rows are what the step waits for.
 constexpr int kTerms = 3;
-template <typename T, class C, int D, class SeeFn, class LiveFn, class KsFn, class VsFn>
-__device__ __forceinline__ void attend(Stage<C, D>& st, const Query<T, C, D>& q, State<D>& a, bool masked, SeeFn see, LiveFn live, KsFn ks, VsFn vs) {
+// `next_k` and `next_v` request the rows of the wave's next step as soon as this step's are no longer needed.
+template <typename T, class C, int D, class SeeFn, class LiveFn, class KsFn, class VsFn, class NextK, class NextV>
+__device__ __forceinline__ void attend(Stage<C, D>& st, const Query<T, C, D>& q, State<D>& a, bool masked, SeeFn see, LiveFn live, KsFn ks, VsFn vs,
+                                       NextK next_k, NextV next_v) {
   float s[2][4];
   float mx = kNegBig;
 #pragma unroll
@@ -276,6 +360,8 @@ __device__ __forceinline__ void attend(Stage<C, D>& st, const Query<T, C, D>& q,
 #pragma unroll
     for (int i = 0; i < 4; ++i) s[tl][i] = acc[i] * ks(tl, i);
   }
+  next_k();
+  PQC_LOADS_ISSUED();
   if (masked) {
 #pragma unroll
     for (int tl = 0; tl < 2; ++tl)
@@ -338,6 +424,8 @@ __device__ __forceinline__ void attend(Stage<C, D>& st, const Query<T, C, D>& q,
       a.o[2 * j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, p[t], a.o[2 * j + 1], 0, 0, 0);
     }
   }
+  next_v();
+  PQC_LOADS_ISSUED();
 }
 
 __device__ __forceinline__ void store_out(const Geometry& g, void* out, size_t at, float x) {
@@ -347,208 +435,348 @@ __device__ __forceinline__ void store_out(const Geometry& g, void* out, size_t a
     static_cast<float*>(out)[at] = x;
 }
 
-// Attention of one tile of up to 16 query rows over one split of its tokens.  Four waves take 32 tokens each in turn, with a
-// softmax state of their own, folded at the end.  A tile of more than one split leaves (m, l, O) in `partials`, per (slot, head)
-// O[R G][D], then m and l of every row.
+// A barrier for LDS alone: loads from memory stay in flight across it.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+constexpr size_t rows_static_lds(int dim) { return 4 * kStaged * 4 + (size_t)kWaves * kRows * (dim + 2) * 4 + 8; }
+
+// A stretch of a tile: as much of a worker's part of it as has its pages in LDS at a time.
+struct Stretch {
+  Border t;
+  bool begins, ends;  // the worker begins the tile, ends it
+  int most;           // tokens that some query of the tile sees
+  int from, to, stop; // tokens of the stretch, end of the worker's part
+};
+
+// Attention of tiles of up to 16 query rows.  Each workgroup goes through its share of the head's tiles; four waves take 32 tokens
+// of a tile each in turn, with a softmax state of their own, folded at the tile's end.  What a workgroup has of a tile that it does not
+// finish, or not begin, goes to `partials` as (O, m, l): place 2 w + 1 of worker w for a tile that it begins, 2 w for one that it goes on with.
+// Loads never stop at a stretch's end: the next one's pages are looked up while this one is computed, and its first rows are
+// requested before this one's waves are folded.
 // LISTED: one query token per sequence, over the tokens that idx names; entries outside the sequence are left out.
 template <typename T, class C, int D, bool LISTED>
 __global__ __launch_bounds__(256, 2) void attn_rows_kernel(Geometry g, Cache c, const T* __restrict__ q, const int* __restrict__ offsets,
                                                            const int* __restrict__ idx, int n_idx, void* __restrict__ out, float* __restrict__ partials) {
-  __shared__ int place[kStaged];  // page of the split, or row of the listed token; negative: none
+  __shared__ int place[2][kStaged];  // page, or row of the listed token; negative: none
   __shared__ float kscale[kStaged], vscale[kStaged];
   __shared__ float red_o[kWaves][kRows][D];
   __shared__ float red_m[kWaves][kRows], red_l[kWaves][kRows];
-  const int lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4, wave = threadIdx.x >> 6;
-  const int h = blockIdx.y;
-  Item it;
-  if constexpr (LISTED) {
-    it.b = blockIdx.x / g.n_split;
-    it.split = blockIdx.x - it.b * g.n_split;
-    it.n_split = g.n_split;
-    it.tokens = g.split;
-    it.tile = 0;
-    it.slot = g.n_split > 1 ? it.b * g.n_split : -1;
-    it.s = seq_of(g, c.lengths, nullptr, it.b);
-  } else {
-    it = find_item<false>(g, c.lengths, offsets, blockIdx.x);
-    if (it.b < 0) return;
-  }
-  const int qi = it.tile * g.R + col / g.G;  // the lane's query token
-  const bool row_ok = col < g.R * g.G && qi < it.s.nq;
-  const int hidden = it.s.len - it.s.nq;     // tokens in front of the first query's own
-  // tokens that the lane's query, the tile's first and its last query see
-  const int lim = row_ok ? max(LISTED ? n_idx : hidden + qi + 1, 0) : 0;
-  const int most = LISTED ? n_idx : max(hidden + min((it.tile + 1) * g.R, it.s.nq), 0);
-  const int least = LISTED ? n_idx : max(hidden + it.tile * g.R + 1, 0);
-  Query<T, C, D> qf;
-  qf.load(row_ok ? q + ((size_t)(it.s.first + qi) * g.Hq + (size_t)h * g.G + col % g.G) * D : nullptr, quad);
-  State<D> a;
-  a.init();
-  const int t0 = it.split * it.tokens, t1 = it.n_split == 1 ? most : min(t0 + it.tokens, most);
-  const int* table = c.table + (size_t)it.b * g.max_pages;
-  const size_t row_bytes = (size_t)D * C::kBytes;
+  __shared__ int missing[2];  // a page of the stretch is not there
+  constexpr int kPer = kStaged / 256;
   constexpr bool kScaled = C::kBytes == 1;
-  // (an even number of pages: a segment is a multiple of 32 tokens)
-  const int seg_tokens = LISTED ? kStaged : ((kStaged - 2) << g.shift);
-  for (int seg = t0; seg < t1; seg += seg_tokens) {
-    const int seg_end = min(seg + seg_tokens, t1);
-    const int p0 = seg >> g.shift, staged = LISTED ? seg_end - seg : ((seg_end - 1) >> g.shift) - p0 + 1;
-    __syncthreads();
-    bool bad = false;
-    for (int i = threadIdx.x; i < staged; i += 256) {
-      int page = -1, row = 0;
-      if constexpr (LISTED) {
-        const int t = idx[((size_t)it.b * g.Hkv + h) * n_idx + seg + i];
-        if (t >= 0 && t < it.s.len) page = table[t >> g.shift];
-        row = t & (g.P - 1);
-      } else {
-        page = table[p0 + i];
-      }
-      const bool ok = page >= 0 && page < g.n_pages;
-      bad |= !ok;
-      place[i] = !ok ? -1 : LISTED ? ((page * g.Hkv + h) << g.shift) + row : page;
-      kscale[i] = ok ? g.scale_log2e * (kScaled ? c.ks[(size_t)page * g.Hkv + h] : 1.0f) : 0.0f;
-      vscale[i] = ok ? (kScaled ? c.vs[(size_t)page * g.Hkv + h] : 1.0f) : 0.0f;
+  const int lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // scalar, and so are the addresses of the wave's pages
+  const int worker = blockIdx.x / g.Hkv, h = blockIdx.x - worker * g.Hkv;
+  const int rows = g.R * g.G;
+  const size_t row_bytes = (size_t)D * C::kBytes;
+  const int my_token = col / g.G, my_head = col - my_token * g.G;
+  int total, share;
+  Stretch now;
+  now.t = border_of(g, c.lengths, offsets, LISTED ? n_idx : -1, worker, total, share);
+  if (now.t.b >= g.B) return;
+  const int x_end = min((worker + 1) * share, total);
+  // (an even number of pages: a stretch is a multiple of 32 tokens)
+  const int most_staged = LISTED ? kStaged : ((kStaged - 2) << g.shift);
+  // the worker's part of tile y.t; false: it has none
+  auto enter = [&](Stretch& y) {
+    y.begins = y.t.unit == 0;
+    y.ends = x_end >= y.t.at + y.t.units;
+    const int last = y.ends ? 0 : max(x_end - y.t.at - kTileCost, 0);
+    if (!y.ends && y.begins && last == 0) return false;
+    const int hidden = y.t.s.len - y.t.s.nq;
+    y.most = LISTED ? n_idx : max(hidden + min((y.t.tile + 1) * g.R, y.t.s.nq), 0);
+    y.from = y.t.unit * g.grain;
+    y.stop = y.ends ? y.most : min(last * g.grain, y.most);
+    y.to = min(y.from + most_staged, y.stop);
+    return true;
+  };
+  auto advance = [&](Stretch& y) {
+    if (y.to < y.stop) {
+      y.from = y.to;
+      y.to = min(y.from + most_staged, y.stop);
+      return true;
     }
-    const bool any_bad = __syncthreads_or(bad);
-    auto at = [&](int t) { return LISTED ? min(t - seg, staged - 1) : min((t >> g.shift) - p0, staged - 1); };
-    auto issue = [&](Stage<C, D>& st, int t) {
+    y.t.at += y.t.units;
+    if (y.t.at >= x_end) return false;
+    if (y.t.tile + 1 < y.t.tiles) {
+      ++y.t.tile;
+    } else {
+      do {  // the next sequence that has a query
+        if (++y.t.b >= g.B) return false;
+        y.t.s = seq_of(g, c.lengths, LISTED ? nullptr : offsets, y.t.b);
+        y.t.units = tile_units(g, y.t.s, LISTED ? n_idx : -1, y.t.tiles);
+      } while (y.t.tiles == 0);
+      y.t.tile = 0;
+    }
+    y.t.unit = 0;
+    return enter(y);
+  };
+  int raw[kPer];  // entries of the page table or of the list
+  auto look_up = [&](const Stretch& y) {
+    const int p0 = y.from >> g.shift, n = LISTED ? y.to - y.from : ((y.to - 1) >> g.shift) - p0 + 1;
+    const int* at = LISTED ? idx + ((size_t)y.t.b * g.Hkv + h) * n_idx + y.from : c.table + (size_t)y.t.b * g.max_pages + p0;
+    if constexpr (LISTED) {
+      if (y.from >= n_idx) at = idx;  // (an empty stretch reads some entry)
+    }
 #pragma unroll
-      for (int tl = 0; tl < 2; ++tl) {
-        const int tt = t + 16 * tl;
-        if constexpr (LISTED) {
-          const unsigned char* kp = c.k + (size_t)max(place[at(tt + col)], 0) * row_bytes;
+    for (int e = 0; e < kPer; ++e) raw[e] = at[max(min((int)threadIdx.x + 256 * e, n - 1), 0)];
+  };
+  float ks[kPer], vs[kPer];
+  auto put_places = [&](const Stretch& y, int buf) {
+    int row[kPer];
+    if constexpr (LISTED) {
+      const int* table = c.table + (size_t)y.t.b * g.max_pages;
 #pragma unroll
-          for (int j = 0; j < C::template kLoads<D>; ++j) st.k[tl][j] = *reinterpret_cast<const u32x4_t*>(kp + C::load_dim(j, quad) * C::kBytes);
+      for (int e = 0; e < kPer; ++e) {
+        const int t = raw[e];
+        row[e] = t & (g.P - 1);
+        raw[e] = t >= 0 && t < y.t.s.len ? table[t >> g.shift] : -1;
+      }
+    }
+    bool bad = false;
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            load_words(c.v + (size_t)max(place[at(tt + 4 * quad + i)], 0) * row_bytes + col * (D / 16) * C::kBytes, st.v[4 * tl + i]);
+    for (int e = 0; e < kPer; ++e) {
+      const bool ok = raw[e] >= 0 && raw[e] < g.n_pages;
+      bad |= !ok;
+      const size_t p = (size_t)(ok ? raw[e] : 0) * g.Hkv + h;
+      ks[e] = kScaled ? c.ks[p] : 1.0f;
+      vs[e] = kScaled ? c.vs[p] : 1.0f;
+      place[buf][threadIdx.x + 256 * e] = !ok ? -1 : LISTED ? (int)(p << g.shift) + row[e] : raw[e];
+      if (!ok) ks[e] = vs[e] = 0.0f;
+    }
+    if (bad) missing[buf] = 1;
+  };
+  auto at = [&](const Stretch& y, int t) { return LISTED ? t - y.from : (t >> g.shift) - (y.from >> g.shift); };
+  Stage<C, D> st;
+  auto issue_k = [&](const Stretch& y, int buf, int t) {
+#pragma unroll
+    for (int tl = 0; tl < 2; ++tl) {
+      const int tt = t + 16 * tl;
+      if constexpr (LISTED) {
+        const unsigned char* kp = c.k + (size_t)max(place[buf][at(y, tt + col)], 0) * row_bytes;
+#pragma unroll
+        for (int j = 0; j < C::template kLoads<D>; ++j) st.k[tl][j] = *reinterpret_cast<const u32x4_t*>(kp + C::load_dim(j, quad) * C::kBytes);
+      } else {
+        const int pg = __builtin_amdgcn_readfirstlane(max(place[buf][at(y, tt)], 0));
+        const unsigned char* kp = c.k + ((((size_t)pg * g.Hkv + h) << g.shift) + (tt & (g.P - 1))) * row_bytes;
+#pragma unroll
+        for (int j = 0; j < C::template kLoads<D>; ++j)
+          st.k[tl][j] = *reinterpret_cast<const u32x4_t*>(kp + (unsigned)((col * D + C::load_dim(j, quad)) * C::kBytes));
+      }
+    }
+  };
+  auto issue_v = [&](const Stretch& y, int buf, int t) {
+#pragma unroll
+    for (int tl = 0; tl < 2; ++tl) {
+      const int tt = t + 16 * tl;
+      if constexpr (LISTED) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          load_words(c.v + (size_t)max(place[buf][at(y, tt + 4 * quad + i)], 0) * row_bytes + col * (D / 16) * C::kBytes, st.v[4 * tl + i]);
+      } else {
+        const int pg = __builtin_amdgcn_readfirstlane(max(place[buf][at(y, tt)], 0));
+        const unsigned char* vp = c.v + ((((size_t)pg * g.Hkv + h) << g.shift) + (tt & (g.P - 1))) * row_bytes;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) load_words(vp + (unsigned)(((4 * quad + i) * D + col * (D / 16)) * C::kBytes), st.v[4 * tl + i]);
+      }
+    }
+  };
+  auto first_rows = [&](const Stretch& y, int buf) {
+    const int t = y.from + wave * kStep;
+    if (t < y.to) {
+      issue_k(y, buf, t);
+      issue_v(y, buf, t);
+    }
+    PQC_LOADS_ISSUED();
+  };
+  if (!enter(now)) return;
+  Query<T, C, D> qf;
+  State<D> a;
+  int lim = 0, least = 0;
+  look_up(now);
+  if (threadIdx.x < 2) missing[threadIdx.x] = 0;
+  __syncthreads();
+  put_places(now, 0);
+  lds_barrier();
+  first_rows(now, 0);
+  bool fresh = true;  // a tile begins
+  for (int buf = 0;; buf ^= 1) {
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+      kscale[threadIdx.x + 256 * e] = ks[e] * g.scale_log2e;
+      vscale[threadIdx.x + 256 * e] = vs[e];
+    }
+    if (threadIdx.x == 0) missing[buf ^ 1] = 0;
+    Stretch next = now;
+    const bool more = advance(next);
+    if (more) look_up(next);
+    if (fresh) {
+      const Seq& s = now.t.s;
+      const int qi = now.t.tile * g.R + my_token;  // the lane's query token
+      const bool row_ok = col < rows && qi < s.nq;
+      // tokens that the lane's query and the tile's first one see
+      lim = row_ok ? max(LISTED ? n_idx : s.len - s.nq + qi + 1, 0) : 0;
+      least = LISTED ? n_idx : max(s.len - s.nq + now.t.tile * g.R + 1, 0);
+      qf.load(row_ok ? q + ((size_t)(s.first + qi) * g.Hq + (size_t)h * g.G + my_head) * D : nullptr, quad);
+      a.init();
+    }
+    lds_barrier();
+    const bool any_missing = missing[buf] != 0;
+    const int most = now.most;
+    for (int t = now.from + wave * kStep; t < now.to; t += kGrain) {
+      const bool again = t + kGrain < now.to;
+      auto token = [&](int tl, int i) { return t + 16 * tl + 4 * quad + i; };
+      auto slot = [&](int tl, int i) { return at(now, LISTED ? token(tl, i) : t + 16 * tl); };
+      attend<T, C, D>(
+          st, qf, a, any_missing || t + kStep > least, [&](int tl, int i) { return token(tl, i) < lim && place[buf][slot(tl, i)] >= 0; },
+          [&](int tl, int i) { return token(tl, i) < most && place[buf][slot(tl, i)] >= 0; }, [&](int tl, int i) { return kscale[slot(tl, i)]; },
+          [&](int tl, int i) { return vscale[slot(tl, i)]; },
+          [&]() {
+            if (again) issue_k(now, buf, t + kGrain);
+          },
+          [&]() {
+            if (again) issue_v(now, buf, t + kGrain);
+          });
+    }
+    if (more) put_places(next, buf ^ 1);
+    lds_barrier();
+    if (more) first_rows(next, buf ^ 1);
+    fresh = now.to >= now.stop;
+    if (fresh) {  // fold the waves
+      const float l = quad_sum(a.l);
+      if (quad == 0) {
+        red_m[wave][col] = a.m;
+        red_l[wave][col] = l;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int n = 0; n < D / 16; ++n) red_o[wave][col][D / 16 * (4 * quad + i) + n] = a.o[n][i];
+      lds_barrier();
+      float* po = partials + ((size_t)(2 * worker + (now.begins ? 1 : 0)) * g.Hkv + h) * partial_floats(rows, D);
+      for (int i = threadIdx.x; i < rows * D; i += 256) {
+        const int r = i / D, d = i % D;
+        float m = red_m[0][r], sum = 0.0f, o = 0.0f;
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) m = fmaxf(m, red_m[w][r]);
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+          const float f = __builtin_amdgcn_exp2f(red_m[w][r] - m);
+          sum += f * red_l[w][r];
+          o += f * red_o[w][r][d];
+        }
+        if (!now.begins || !now.ends) {
+          po[i] = o;
+          if (d == 0) {
+            po[rows * D + 2 * r] = m;
+            po[rows * D + 2 * r + 1] = sum;
+          }
         } else {
-          const int page = __builtin_amdgcn_readfirstlane(max(place[at(tt)], 0));
-          const size_t base = ((((size_t)page * g.Hkv + h) << g.shift) + (tt & (g.P - 1))) * row_bytes;
-          const unsigned char *kp = c.k + base, *vp = c.v + base;
-#pragma unroll
-          for (int j = 0; j < C::template kLoads<D>; ++j)
-            st.k[tl][j] = *reinterpret_cast<const u32x4_t*>(kp + (col * D + C::load_dim(j, quad)) * C::kBytes);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) load_words(vp + ((4 * quad + i) * D + col * (D / 16)) * C::kBytes, st.v[4 * tl + i]);
+          const int qr = now.t.tile * g.R + r / g.G;
+          if (qr < now.t.s.nq) store_out(g, out, ((size_t)(now.t.s.first + qr) * g.Hq + (size_t)h * g.G + r % g.G) * D + d, sum > 0.0f ? o / sum : 0.0f);
         }
       }
-    };
-    auto consume = [&](Stage<C, D>& st, int t) {
-      auto token = [&](int tl, int i) { return t + 16 * tl + 4 * quad + i; };
-      auto slot = [&](int tl, int i) { return at(LISTED ? token(tl, i) : t + 16 * tl); };
-      attend<T, C, D>(
-          st, qf, a, any_bad || t + kStep > least, [&](int tl, int i) { return token(tl, i) < lim && place[slot(tl, i)] >= 0; },
-          [&](int tl, int i) { return token(tl, i) < most && place[slot(tl, i)] >= 0; }, [&](int tl, int i) { return kscale[slot(tl, i)]; },
-          [&](int tl, int i) { return vscale[slot(tl, i)]; });
-    };
-    Stage<C, D> sa, sb;
-    int t = seg + wave * kStep;
-    if (t < seg_end) {
-      issue(sa, t);
-      for (;;) {  // the next step's loads travel while this one is computed; past the end the last rows are read again
-        const int n1 = min(t + kGrain, (seg_end - 1) & ~(kStep - 1));
-        issue(sb, n1);
-        PQC_LOADS_ISSUED();
-        consume(sa, t);
-        t += kGrain;
-        if (t >= seg_end) break;
-        issue(sa, min(t + kGrain, (seg_end - 1) & ~(kStep - 1)));
-        PQC_LOADS_ISSUED();
-        consume(sb, t);
-        t += kGrain;
-        if (t >= seg_end) break;
-      }
     }
-  }
-  // fold the waves
-  const float l = quad_sum(a.l);
-  if (quad == 0) {
-    red_m[wave][col] = a.m;
-    red_l[wave][col] = l;
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int n = 0; n < D / 16; ++n) red_o[wave][col][D / 16 * (4 * quad + i) + n] = a.o[n][i];
-  __syncthreads();
-  const int rows = g.R * g.G;
-  float* po = partials + ((size_t)(it.slot + it.split) * g.Hkv + h) * (size_t)(rows * (D + 2));
-  for (int i = threadIdx.x; i < rows * D; i += 256) {
-    const int r = i / D, d = i % D;
-    float m = red_m[0][r], sum = 0.0f, o = 0.0f;
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w) m = fmaxf(m, red_m[w][r]);
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      const float f = __builtin_amdgcn_exp2f(red_m[w][r] - m);
-      sum += f * red_l[w][r];
-      o += f * red_o[w][r][d];
-    }
-    if (it.slot >= 0) {
-      po[i] = o;
-      if (d == 0) {
-        po[rows * D + 2 * r] = m;
-        po[rows * D + 2 * r + 1] = sum;
-      }
-    } else {
-      const int qr = it.tile * g.R + r / g.G;
-      if (qr < it.s.nq) store_out(g, out, ((size_t)(it.s.first + qr) * g.Hq + (size_t)h * g.G + r % g.G) * D + d, sum > 0.0f ? o / sum : 0.0f);
-    }
+    if (!more) return;
+    now = next;
   }
 }
 
-// Folds the splits of a tile: one workgroup per (tile, head, row).
-template <int D, bool LISTED>
-__global__ __launch_bounds__(256) void attn_merge_kernel(Geometry g, const int* __restrict__ lengths, const int* __restrict__ offsets,
+// Folds the parts of a tile in one pass: D / 4 lanes per row and part, PARTS parts of the splits of a row side by side (eight where
+// a tile is cut into many splits, one where it has many rows and few splits), each with a running maximum.
+template <int D, bool ROWS, int PARTS>
+__global__ __launch_bounds__(256) void attn_merge_kernel(Geometry g, const int* __restrict__ lengths, const int* __restrict__ offsets, int listed,
                                                          const float* __restrict__ partials, void* __restrict__ out) {
-  constexpr int kGroups = 256 / D;
-  __shared__ float wave_m[4], red_o[kGroups][D], red_l[kGroups];
+  constexpr int kLanes = D / 4, kGroups = 256 / kLanes, kAtOnce = kGroups / PARTS;
+  __shared__ f32x4_t red_o[kGroups][kLanes];
+  __shared__ float2 red_ml[kGroups];
   const int h = blockIdx.y;
   Item it;
-  if constexpr (LISTED) {
-    it.b = blockIdx.x;
-    it.n_split = g.n_split;
-    it.tile = 0;
-    it.slot = it.b * g.n_split;
-    it.s = Seq{it.b, 1, 0};
+  if constexpr (ROWS) {
+    // the first border inside a tile stands for it: its parts are those of the worker in front and of all that begin inside it
+    const int w = blockIdx.x + 1;
+    int total, share;
+    const Border e = border_of(g, lengths, offsets, listed, w, total, share);
+    if (e.b >= g.B || e.unit == 0) return;
+    if ((w - 1) * share > e.at + kTileCost) return;  // not the first
+    it.b = e.b;
+    it.tile = e.tile;
+    it.slot = w - 1;
+    it.n_split = (e.at + e.units - 1) / share - (w - 1) + 1;
+    it.s = e.s;
   } else {
     it = find_item<true>(g, lengths, offsets, blockIdx.x);
     if (it.b < 0) return;
   }
   const int rows = g.R * g.G;
-  const size_t stride = (size_t)g.Hkv * rows * (D + 2);
-  const float* base = partials + ((size_t)it.slot * g.Hkv + h) * (size_t)(rows * (D + 2));
-  const int d = threadIdx.x % D, part = threadIdx.x / D;
-  for (int r = blockIdx.z; r < rows; r += gridDim.z) {
+  const size_t one = partial_floats(rows, D), stride = (size_t)g.Hkv * one;
+  const float* base = partials + ((size_t)it.slot * g.Hkv + h) * one;
+  auto part_at = [&](int i) {  // ROWS: place 2 w + 1 of the worker that begins the tile, 2 w of those that go on
+    return ROWS ? partials + ((size_t)(2 * (it.slot + i) + (i == 0 ? 1 : 0)) * g.Hkv + h) * one : base + (size_t)i * stride;
+  };
+  const int at = threadIdx.x % kLanes, group = threadIdx.x / kLanes, part = group % PARTS;
+  for (int r0 = blockIdx.z * kAtOnce; r0 < rows; r0 += gridDim.z * kAtOnce) {
+    const int r = r0 + group / PARTS;
     const int qr = it.tile * g.R + r / g.G;
-    if (qr >= it.s.nq) return;
-    float m = kNegBig;
-    for (int i = threadIdx.x; i < it.n_split; i += 256) m = fmaxf(m, base[i * stride + rows * D + 2 * r]);
-    m = wave_max(m);
-    __syncthreads();  // the row before has been read
-    if ((threadIdx.x & 63) == 0) wave_m[threadIdx.x >> 6] = m;
-    __syncthreads();
-    m = fmaxf(fmaxf(wave_m[0], wave_m[1]), fmaxf(wave_m[2], wave_m[3]));
-    float o = 0.0f, l = 0.0f;
-#pragma unroll 4
-    for (int i = part; i < it.n_split; i += kGroups) {
-      const float* p = base + i * stride;
-      const float f = __builtin_amdgcn_exp2f(p[rows * D + 2 * r] - m);
-      l += f * p[rows * D + 2 * r + 1];
-      o += f * p[r * D + d];
-    }
-    red_o[part][d] = o;
-    if (d == 0) red_l[part] = l;
-    __syncthreads();
-    if (part == 0) {
+    f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+    float m = kNegBig, l = 0.0f;
+    if (r < rows && qr < it.s.nq) {
+      constexpr int kAhead = 8;
+      for (int i = part; i < it.n_split; i += kAhead * PARTS) {
+        float2 ml[kAhead];
+        f32x4_t x[kAhead];
 #pragma unroll
-      for (int i = 1; i < kGroups; ++i) {
-        o += red_o[i][d];
-        l += red_l[i];
+        for (int e = 0; e < kAhead; ++e) {  // past the end the last split is read again and left out
+          const float* p = part_at(min(i + e * PARTS, it.n_split - 1));
+          ml[e] = *reinterpret_cast<const float2*>(p + rows * D + 2 * r);
+          x[e] = *reinterpret_cast<const f32x4_t*>(p + r * D + 4 * at);
+          if (i + e * PARTS >= it.n_split) ml[e] = make_float2(-INFINITY, 0.0f);
+        }
+        float mnew = m;
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) mnew = fmaxf(mnew, ml[e].x);
+        const float corr = __builtin_amdgcn_exp2f(m - mnew);
+        m = mnew;
+        l *= corr;
+        o *= corr;
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) {
+          const float f = __builtin_amdgcn_exp2f(ml[e].x - m);
+          l += f * ml[e].y;
+          o += f * x[e];
+        }
       }
-      store_out(g, out, ((size_t)(it.s.first + qr) * g.Hq + (size_t)h * g.G + r % g.G) * D + d, l > 0.0f ? o / l : 0.0f);
+    }
+    if constexpr (PARTS > 1) {
+      __syncthreads();  // the rows before have been read
+      red_o[group][at] = o;
+      if (at == 0) red_ml[group] = make_float2(m, l);
+      __syncthreads();
+      if (part == 0) {
+#pragma unroll
+        for (int e = 1; e < PARTS; ++e) m = fmaxf(m, red_ml[group + e].x);
+        l = 0.0f;
+        o = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int e = 0; e < PARTS; ++e) {
+          const float f = __builtin_amdgcn_exp2f(red_ml[group + e].x - m);
+          l += f * red_ml[group + e].y;
+          o += f * red_o[group + e][at];
+        }
+      }
+    }
+    if (part == 0 && r < rows && qr < it.s.nq) {
+      const size_t a = ((size_t)(it.s.first + qr) * g.Hq + (size_t)h * g.G + r % g.G) * D + 4 * at;
+      const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+      o *= inv;
+      if (g.out_bf16)
+        *reinterpret_cast<u32x2_t*>(static_cast<bf16_t*>(out) + a) = u32x2_t{pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};
+      else
+        *reinterpret_cast<f32x4_t*>(static_cast<float*>(out) + a) = o;
     }
   }
 }
@@ -665,7 +893,7 @@ __global__ __launch_bounds__(256, 2) void attn_block_kernel(Geometry g, Cache c,
                                                             void* __restrict__ out, float* __restrict__ partials) {
   __shared__ __align__(16) unsigned char lds_k[2][kBlockTokens * D * 2], lds_v[2][kBlockTokens * D * 2];
   __shared__ unsigned present[2];  // a byte per 16 tokens: their page is there
-  const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, half = lane >> 5, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // the heads of a KV head's tokens follow each other, so that with eight of them an XCD's L2 holds the rows of one
   const int item = blockIdx.x / g.Hkv, h = blockIdx.x - item * g.Hkv;
   const Item it = find_item<false>(g, c.lengths, offsets, item);
@@ -796,7 +1024,7 @@ __global__ __launch_bounds__(256, 2) void attn_block_kernel(Geometry g, Cache c,
   if (r >= g.R * g.G) return;
   if (it.slot >= 0) {
     const int rows = g.R * g.G;
-    float* po = partials + ((size_t)(it.slot + it.split) * g.Hkv + h) * (size_t)(rows * (D + 2));
+    float* po = partials + ((size_t)(it.slot + it.split) * g.Hkv + h) * partial_floats(rows, D);
 #pragma unroll
     for (int n = 0; n < D / 32; ++n)
 #pragma unroll
@@ -896,64 +1124,99 @@ __device__ __forceinline__ float power_scale(float amax) {
   return __uint_as_float((unsigned)(e + 127) << 23);
 }
 
-// Rotated values of dimensions 8 c .. 8 c + 7 of a head at `p`.  Every product and sum is rounded by itself.
-template <typename T>
-__device__ __forceinline__ void rotate8(const AppendArgs& a, const T* p, int c, int pos, float (&y)[8]) {
-#pragma clang fp contract(off)
-  float x[8];
-  load8(p + 8 * c, x);
-  const int half = a.rot >> 1;
-  if (8 * c >= a.rot) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = x[i];
-    return;
+// A thread has sixteen dimensions of a head: part j of D / 16.  Rotated ones are eight pairs, 8 j .. 8 j + 7, in halves
+// (dimensions 8 j.. and rot / 2 + 8 j..) or next to each other (16 j..); behind the rotated parts come sixteen adjacent ones.
+struct Dims {
+  int lo, hi;    // the two groups of eight
+  bool rotated;
+};
+__device__ __forceinline__ Dims dims_of(const AppendArgs& a, int j) {
+  const bool rotated = 16 * j < a.rot;
+  const bool halves = rotated && !a.pairs;
+  return Dims{halves ? 8 * j : 16 * j, halves ? 8 * j + (a.rot >> 1) : 16 * j + 8, rotated};
+}
+struct Angles {
+  float co[8], si[8];
+  __device__ __forceinline__ void load(const AppendArgs& a, int j, int pos) {
+    const float* row = a.table + (size_t)min(max(pos, 0), a.rot_positions - 1) * a.rot + 8 * j;
+    load8(row, co);
+    load8(row + (a.rot >> 1), si);
   }
-  const float* row = a.table + (size_t)min(max(pos, 0), a.rot_positions - 1) * a.rot;
+};
+// Every product and sum is rounded by itself.
+__device__ __forceinline__ void rotate(const AppendArgs& a, const Angles& w, float (&lo)[8], float (&hi)[8]) {
+#pragma clang fp contract(off)
   if (a.pairs) {
-    const f32x4_t co = *reinterpret_cast<const f32x4_t*>(row + 4 * c), si = *reinterpret_cast<const f32x4_t*>(row + half + 4 * c);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      y[2 * i] = x[2 * i] * co[i] - x[2 * i + 1] * si[i];
-      y[2 * i + 1] = x[2 * i + 1] * co[i] + x[2 * i] * si[i];
+      float x = lo[2 * i], y = lo[2 * i + 1];
+      lo[2 * i] = x * w.co[i] - y * w.si[i];
+      lo[2 * i + 1] = y * w.co[i] + x * w.si[i];
+      x = hi[2 * i];
+      y = hi[2 * i + 1];
+      hi[2 * i] = x * w.co[4 + i] - y * w.si[4 + i];
+      hi[2 * i + 1] = y * w.co[4 + i] + x * w.si[4 + i];
     }
   } else {
-    const bool low = 8 * c < half;
-    const int j = 8 * c - (low ? 0 : half);
-    float z[8], co[8], si[8];
-    load8(p + (low ? 8 * c + half : j), z);
-    load8(row + j, co);
-    load8(row + half + j, si);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = low ? x[i] * co[i] - z[i] * si[i] : x[i] * co[i] + z[i] * si[i];
+    for (int i = 0; i < 8; ++i) {
+      const float x = lo[i], y = hi[i];
+      lo[i] = x * w.co[i] - y * w.si[i];
+      hi[i] = y * w.co[i] + x * w.si[i];
+    }
+  }
+}
+
+// Queries of a.q_tokens tokens: a thread goes through the heads of one token with the same angles, which are read once.
+template <typename T, int D>
+__device__ __forceinline__ void append_queries(const Geometry& g, const Cache& c, const AppendArgs& a, const int* __restrict__ offsets, int group) {
+  constexpr int kParts = D / 16, kSlots = 256 / kParts;
+  const int j = threadIdx.x % kParts, slot = threadIdx.x / kParts;
+  const int heads_at_once = kSlots / a.q_tokens;
+  const int t = group * a.q_tokens + slot / heads_at_once;
+  if (t >= g.n_q) return;
+  int b = t, begin = t, end = t + 1;
+  if (offsets) {  // the sequence of token t: the offsets ascend
+    int lo = 0, hi = g.B;  // the first b whose end is beyond t
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (offsets[mid + 1] <= t)
+        lo = mid + 1;
+      else
+        hi = mid;
+    }
+    b = lo;
+    if (b >= g.B) return;  // behind the last sequence: left as it is
+    begin = offsets[b];
+    end = offsets[b + 1];
+    if (t < begin) return;
+  }
+  const Dims d = dims_of(a, j);
+  Angles w;
+  if (d.rotated) w.load(a, j, a.positions ? a.positions[t] : token_count(c.lengths[b]) - (end - t));
+  const T* src = static_cast<const T*>(a.q) + (size_t)t * a.q_stride;
+  T* dst = static_cast<T*>(a.q_out) + (size_t)t * g.Hq * D;
+#pragma unroll 4
+  for (int h = slot % heads_at_once; h < g.Hq; h += heads_at_once) {
+    float lo[8], hi[8];
+    load8(src + (size_t)h * D + d.lo, lo);
+    load8(src + (size_t)h * D + d.hi, hi);
+    if (d.rotated) rotate(a, w, lo, hi);
+    store8(dst + (size_t)h * D + d.lo, lo);
+    store8(dst + (size_t)h * D + d.hi, hi);
   }
 }
 
 // One workgroup per (sequence, page that the call touches, head, key or value), and behind them workgroups that rotate queries.
+// Of the page's new tokens a thread keeps up to kHeld parts between the pass that finds the largest value and the one that writes the
+// codes; where there are more the inputs are read again.
 template <typename T, bool FP8, int D>
 __global__ __launch_bounds__(256) void append_kernel(Geometry g, Cache c, AppendArgs a, const int* __restrict__ offsets) {
-  constexpr int kChunks = D / 8;
+  constexpr int kParts = D / 16, kSlots = 256 / kParts, kHeld = 2;
   const int tid = threadIdx.x, lane = tid & 63;
   const int kv_groups = a.kv_items * 2 * g.Hkv;
-  if ((int)blockIdx.x >= kv_groups) {  // queries
-    const int first = ((int)blockIdx.x - kv_groups) * a.q_tokens;
-    for (int t = first; t < min(first + a.q_tokens, g.n_q); ++t) {
-      int b = t;
-      if (offsets) {  // the sequence of token t: how many end at or before it
-        b = 0;
-        for (int b0 = 0; b0 < g.B; b0 += 64) b += __popcll(__ballot(b0 + lane < g.B && offsets[b0 + lane + 1] <= t));
-      }
-      if (b >= g.B) return;  // behind the last sequence: left as it is
-      const int begin = offsets ? offsets[b] : b, end = offsets ? offsets[b + 1] : b + 1;
-      if (t < begin) continue;
-      const int pos = a.positions ? a.positions[t] : token_count(c.lengths[b]) - (end - t);
-      const T* src = static_cast<const T*>(a.q) + (size_t)t * a.q_stride;
-      T* dst = static_cast<T*>(a.q_out) + (size_t)t * g.Hq * D;
-      for (int i = tid; i < g.Hq * kChunks; i += 256) {
-        float y[8];
-        rotate8(a, src + (size_t)(i / kChunks) * D, i % kChunks, pos, y);
-        store8(dst + (size_t)i * 8, y);
-      }
-    }
+  if ((int)blockIdx.x >= kv_groups) {
+    append_queries<T, D>(g, c, a, offsets, (int)blockIdx.x - kv_groups);
     return;
   }
   const int j = blockIdx.x / (2 * g.Hkv), which = blockIdx.x - j * 2 * g.Hkv;
@@ -994,36 +1257,55 @@ __global__ __launch_bounds__(256) void append_kernel(Geometry g, Cache c, Append
   const int n = stop - start, held = start & (g.P - 1);
   const T* src = static_cast<const T*>(is_key ? a.k : a.v);
   const long long stride = is_key ? a.k_stride : a.v_stride;
-  auto value = [&](int i, int chunk, float (&y)[8]) {  // new token start + i
+  const int part = tid % kParts, slot = tid / kParts;
+  Dims d = dims_of(a, part);
+  if (!is_key && d.rotated) d = Dims{16 * part, 16 * part + 8, false};
+  auto value = [&](int i, float (&lo)[8], float (&hi)[8]) {  // new token start + i
     const int t = first + start + i;
     const T* p = src + (size_t)t * stride + (size_t)h * D;
-    if (is_key && a.rot > 0)
-      rotate8(a, p, chunk, a.positions ? a.positions[t] : start + i, y);
-    else
-      load8(p + 8 * chunk, y);
+    load8(p + d.lo, lo);
+    load8(p + d.hi, hi);
+    if (d.rotated) {
+      Angles w;
+      w.load(a, part, a.positions ? a.positions[t] : start + i);
+      rotate(a, w, lo, hi);
+    }
   };
-  auto key_out = [&](int i, int chunk, const float (&y)[8]) {
-    if (is_key && a.k_out) store8(static_cast<T*>(a.k_out) + ((size_t)(first + start + i) * g.Hkv + h) * D + 8 * chunk, y);
+  auto key_out = [&](int i, const float (&lo)[8], const float (&hi)[8]) {
+    if (!is_key || !a.k_out) return;
+    T* p = static_cast<T*>(a.k_out) + ((size_t)(first + start + i) * g.Hkv + h) * D;
+    store8(p + d.lo, lo);
+    store8(p + d.hi, hi);
   };
   const size_t block = (((size_t)(stored ? page : 0) * g.Hkv + h) << g.shift) * D;
   if constexpr (FP8) {
     __shared__ float wave_max_of[4];
-    float amax = 0.0f;
-    for (int i = tid; i < n * kChunks; i += 256) {
-      float y[8];
-      value(i / kChunks, i % kChunks, y);
+    float* scale = (is_key ? c.ks : c.vs) + (size_t)(stored ? page : 0) * g.Hkv + h;
+    const float old = stored && held > 0 ? *scale : 0.0f;
+    float lo[kHeld][8], hi[kHeld][8], amax = 0.0f;
+    auto largest = [&](const float (&x)[8], const float (&y)[8]) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(y[e]));
+      for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fmaxf(fabsf(x[e]), fabsf(y[e])));
+    };
+#pragma unroll
+    for (int e = 0; e < kHeld; ++e)
+      if (slot + e * kSlots < n) {
+        value(slot + e * kSlots, lo[e], hi[e]);
+        largest(lo[e], hi[e]);
+      }
+    for (int i = slot + kHeld * kSlots; i < n; i += kSlots) {
+      float x[8], y[8];
+      value(i, x, y);
+      largest(x, y);
     }
     amax = wave_max(amax);
     if (lane == 0) wave_max_of[tid >> 6] = amax;
-    __syncthreads();
+    __syncthreads();  // (every wave has read the old scale)
     amax = fmaxf(fmaxf(wave_max_of[0], wave_max_of[1]), fmaxf(wave_max_of[2], wave_max_of[3]));
-    float* scale = (is_key ? c.ks : c.vs) + (size_t)(stored ? page : 0) * g.Hkv + h;
-    const float old = stored && held > 0 ? *scale : 0.0f, want = power_scale(amax), s = fmaxf(old, want);
+    const float want = power_scale(amax), s = fmaxf(old, want);
     unsigned char* codes = (is_key ? c.k : c.v) + block;
     if (stored && held > 0 && s > old) {
-      for (int i = tid; i < held * kChunks; i += 256) {
+      for (int i = tid; i < held * (D / 8); i += 256) {
         float y[8];
         u32x2_t* w = reinterpret_cast<u32x2_t*>(codes + (size_t)i * 8);
         decode8(*w, y);
@@ -1031,21 +1313,33 @@ __global__ __launch_bounds__(256) void append_kernel(Geometry g, Cache c, Append
       }
     }
     const float inv = 1.0f / s;
-    for (int i = tid; i < n * kChunks; i += 256) {
-      float y[8];
-      value(i / kChunks, i % kChunks, y);
-      key_out(i / kChunks, i % kChunks, y);
-      if (stored) *reinterpret_cast<u32x2_t*>(codes + (size_t)held * D + (size_t)i * 8) = encode8(y, inv);
+    auto write = [&](int i, const float (&x)[8], const float (&y)[8]) {
+      key_out(i, x, y);
+      if (stored) {
+        unsigned char* row = codes + (size_t)(held + i) * D;
+        *reinterpret_cast<u32x2_t*>(row + d.lo) = encode8(x, inv);
+        *reinterpret_cast<u32x2_t*>(row + d.hi) = encode8(y, inv);
+      }
+    };
+#pragma unroll
+    for (int e = 0; e < kHeld; ++e)
+      if (slot + e * kSlots < n) write(slot + e * kSlots, lo[e], hi[e]);
+    for (int i = slot + kHeld * kSlots; i < n; i += kSlots) {
+      float x[8], y[8];
+      value(i, x, y);
+      write(i, x, y);
     }
-    __syncthreads();  // every wave has read the old scale
     if (stored && tid == 0) *scale = s;
   } else {
     bf16_t* rows = reinterpret_cast<bf16_t*>(is_key ? c.k : c.v) + block + (size_t)held * D;
-    for (int i = tid; i < n * kChunks; i += 256) {
-      float y[8];
-      value(i / kChunks, i % kChunks, y);
-      key_out(i / kChunks, i % kChunks, y);
-      if (stored) store8(rows + (size_t)i * 8, y);
+    for (int i = slot; i < n; i += kSlots) {
+      float x[8], y[8];
+      value(i, x, y);
+      key_out(i, x, y);
+      if (stored) {
+        store8(rows + (size_t)i * D + d.lo, x);
+        store8(rows + (size_t)i * D + d.hi, y);
+      }
     }
   }
 }
