@@ -410,6 +410,7 @@ typedef struct pqc_paged_cache { /* device pointers, 16-byte aligned (page_table
   float* v_scale;
   const int32_t* page_table;
   const int32_t* lengths;
+  uint32_t* counters;    /* NULL, or pqc_paged_counter_bytes: see there              */
 } pqc_paged_cache;
 
 #define PQC_ROT_HALVES 0 /* dimension j is rotated with j + rot_dims/2  */
@@ -443,6 +444,13 @@ int pqc_paged_append(const pqc_paged_config* cfg, const pqc_paged_cache* cache, 
  * pqc_paged_attn).  Of the configuration's sizes alone, not of what the arrays hold.  0 if the
  * configuration is refused, and where no workspace is needed. */
 size_t pqc_paged_workspace_bytes(const pqc_paged_config* cfg, int32_t n, int32_t n_idx);
+
+/* Where a sequence's tokens are spread over several workgroups, their results are folded by a
+ * launch of its own, or, with `counters` and where they are few, by whichever workgroup ends last,
+ * which saves that launch; the order in which they are added up differs.  counters: this many bytes of device memory, zero before their
+ * first use; a completed call leaves them zero.  Calls that share them must be ordered on one
+ * stream (two graphs that may run at once need counters of their own). */
+size_t pqc_paged_counter_bytes(const pqc_paged_config* cfg);
 
 /* Softmax attention of every query head over all cached tokens of its sequence up to the
  * query's own place (causal): query token i of the m of sequence b sees the tokens

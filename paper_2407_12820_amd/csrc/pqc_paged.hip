@@ -22,6 +22,12 @@ constexpr size_t kRowsLds = 56 * 1024;
 // Items of the kernel of 128 rows that the length of a split aims at.
 constexpr int kBlockItems = 480;
 
+// Parts per tile up to which the last workgroup of a tile folds them itself; beyond that a launch of its own with a workgroup per row
+// is quicker than one workgroup for all rows.  us, folded by the last and by a launch of its own: 8 heads of 4 query heads,
+// 131072 tokens in all, 1 sequence (64 parts) 62.9, 59.4, 2 59.0, 59.5, 4 57.4, 59.8, 32 58.0, 61.8; 4 sequences of 2 heads (64 parts) 34.8,
+// 26.1, 16 24.1, 26.8; listed, 13175 tokens each, 2 sequences of 8 query heads (32 parts) 26.0, 21.9, 4 32.7, 33.7.
+constexpr int kPartsFolded = 16;
+
 int make_geometry(const pqc_paged_config* c, long long n, Geometry* g) {
   if (!c) return PQC_EINVAL;
   if (c->batch < 1 || c->n_q_heads < 1 || c->n_kv_heads < 1 || c->n_q_heads % c->n_kv_heads || c->head_dim < 1 || c->page_tokens < 1 ||
@@ -97,11 +103,12 @@ int check_cache(const pqc_paged_config* cfg, const pqc_paged_cache* c) {
   if (!c || !c->k_pages || !c->v_pages || !c->page_table || !c->lengths) return PQC_EINVAL;
   if (cfg->cache_dtype == PQC_FP8 && (!c->k_scale || !c->v_scale)) return PQC_EINVAL;
   if (!aligned(c->k_pages, 16) || !aligned(c->v_pages, 16) || !aligned(c->page_table, 4) || !aligned(c->lengths, 4)) return PQC_EINVAL;
+  if (!aligned(c->counters, 4)) return PQC_EINVAL;
   if (cfg->cache_dtype == PQC_FP8 && (!aligned(c->k_scale, 16) || !aligned(c->v_scale, 16))) return PQC_EINVAL;
   return PQC_OK;
 }
 Cache device_cache(const pqc_paged_cache* c) {
-  return Cache{static_cast<unsigned char*>(c->k_pages), static_cast<unsigned char*>(c->v_pages), c->k_scale, c->v_scale, c->page_table, c->lengths};
+  return Cache{static_cast<unsigned char*>(c->k_pages), static_cast<unsigned char*>(c->v_pages), c->k_scale, c->v_scale, c->page_table, c->lengths, c->counters};
 }
 int launched() { return hipGetLastError() == hipSuccess ? PQC_OK : PQC_EHIP; }
 
@@ -120,11 +127,14 @@ template <typename T, class C, int D, bool LISTED>
 void launch_rows(const AttnCall& a) {
   const Geometry& g = a.g;
   constexpr size_t lds = kRowsLds - rows_static_lds(D);
-  hipLaunchKernelGGL((attn_rows_kernel<T, C, D, LISTED>), dim3((unsigned)(g.workers * g.Hkv)), dim3(256), lds, a.st, g, a.c,
+  Cache c = a.c;
+  const int tokens = LISTED ? a.n_idx : g.max_pages << g.shift;
+  if (std::min(g.workers / g.B, tokens / g.grain) > kPartsFolded) c.counters = nullptr;
+  hipLaunchKernelGGL((attn_rows_kernel<T, C, D, LISTED>), dim3((unsigned)(g.workers * g.Hkv)), dim3(256), lds, a.st, g, c,
                      static_cast<const T*>(a.q), a.offsets, a.idx, a.n_idx, a.out, a.partials);
-  if (g.workers > 1 && g.slots > 0)
-    hipLaunchKernelGGL((attn_merge_kernel<D, true, 8>), dim3((unsigned)g.workers - 1, g.Hkv, g.R * g.G), dim3(256), 0, a.st, g, a.c.lengths, a.offsets,
-                       LISTED ? a.n_idx : -1, a.partials, a.out);
+  if (g.workers > 1 && g.slots > 0 && !c.counters)
+    hipLaunchKernelGGL((attn_fold_kernel<C, D>), dim3((unsigned)g.workers - 1, g.Hkv, g.R * g.G), dim3(256), 0, a.st, g, a.c.lengths,
+                       a.offsets,                       LISTED ? a.n_idx : -1, a.partials, a.out);
 }
 template <class C, int D>
 void launch_block(const AttnCall& a) {
@@ -135,8 +145,8 @@ void launch_block(const AttnCall& a) {
   else
     hipLaunchKernelGGL((attn_block_kernel<C, D, 3>), grid, dim3(256), 0, a.st, g, a.c, static_cast<const bf16_t*>(a.q), a.offsets, a.out, a.partials);
   if ((g.max_pages << g.shift) > kGrain)
-    hipLaunchKernelGGL((attn_merge_kernel<D, false, 1>), dim3((unsigned)std::min(g.per_head, g.items - g.per_head), g.Hkv, 4), dim3(256), 0, a.st, g,
-                       a.c.lengths, a.offsets, -1, a.partials, a.out);
+    hipLaunchKernelGGL((attn_block_fold_kernel<D>), dim3((unsigned)std::min(g.per_head, g.items - g.per_head), g.Hkv, 4), dim3(256), 0, a.st, g,
+                       a.c.lengths, a.offsets, a.partials, a.out);
 }
 int launch_blocks(const pqc_paged_config* cfg, const AttnCall& a) {
   if (cfg->cache_dtype == PQC_FP8)
@@ -170,6 +180,13 @@ void launch_append(const Geometry& g, const Cache& c, const AppendArgs& a, const
 }  // namespace
 
 extern "C" {
+
+size_t pqc_paged_counter_bytes(const pqc_paged_config* cfg) {
+  Geometry g;
+  if (make_geometry(cfg, 1, &g) != PQC_OK) return 0;
+  plan_rows(&g, 1, 1);
+  return (size_t)g.workers * g.Hkv * sizeof(unsigned);
+}
 
 size_t pqc_paged_workspace_bytes(const pqc_paged_config* cfg, int32_t n, int32_t n_idx) {
   Geometry g;

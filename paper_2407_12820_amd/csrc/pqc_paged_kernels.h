@@ -38,6 +38,7 @@ struct Cache {
   unsigned char *k, *v;
   float *ks, *vs;
   const int *table, *lengths;
+  unsigned* counters;  // of the parts of tiles, zero between calls; nullptr: parts are folded by a kernel of their own
 };
 
 // A partial result: O[rows][D], then maximum and sum of every row; 16-byte aligned.
@@ -81,9 +82,8 @@ __device__ __forceinline__ int split_tokens(const Geometry& g, const int* length
   const float tokens = ceilf(wave_sum(work) * 1.001f / (float)(g.per_head * kGrain));
   return max(1, (int)fminf(tokens, 1e7f)) * kGrain;
 }
-// The j-th item (MERGE: the j-th tile of more than one split); b < 0: there are fewer.
-template <bool MERGE>
-__device__ __forceinline__ Item find_item(const Geometry& g, const int* lengths, const int* offsets, int j) {
+// The j-th item, or the j-th tile of more than one split (whole_tiles); b < 0: there are fewer.
+__device__ __forceinline__ Item find_item(const Geometry& g, const int* lengths, const int* offsets, int j, bool whole_tiles) {
   Item it;
   it.b = -1;
   it.tokens = split_tokens(g, lengths, offsets);
@@ -100,7 +100,7 @@ __device__ __forceinline__ Item find_item(const Geometry& g, const int* lengths,
     const int mine = n > 1 ? tiles * n : 0;
     const int slot_end = wave_inclusive_scan(mine);
     if (n > 1 && slots + slot_end > g.slots) n = 1;  // (the bound of split_tokens keeps this from happening with offsets that ascend)
-    const int count = MERGE ? (n > 1 ? tiles : 0) : tiles * n;
+    const int count = whole_tiles ? (n > 1 ? tiles : 0) : tiles * n;
     const int end = wave_inclusive_scan(count);
     const unsigned long long has = __ballot(before + end > j);
     if (has) {
@@ -108,9 +108,9 @@ __device__ __forceinline__ Item find_item(const Geometry& g, const int* lengths,
       const int at = j - before - (__builtin_amdgcn_readlane(end, l) - __builtin_amdgcn_readlane(count, l));
       it.b = b0 + l;
       it.n_split = __builtin_amdgcn_readlane(n, l);
-      const int nth = MERGE ? at : at / it.n_split;
+      const int nth = whole_tiles ? at : at / it.n_split;
       it.tile = __builtin_amdgcn_readlane(tiles, l) - 1 - nth;  // the last one, which sees most, first
-      it.split = MERGE ? 0 : at - nth * it.n_split;
+      it.split = whole_tiles ? 0 : at - nth * it.n_split;
       it.slot = it.n_split > 1 ? slots + __builtin_amdgcn_readlane(slot_end - mine, l) + nth * it.n_split : -1;
       it.s.first = __builtin_amdgcn_readlane(s.first, l);
       it.s.nq = __builtin_amdgcn_readlane(s.nq, l);
@@ -231,6 +231,7 @@ __device__ __forceinline__ unsigned pack_bf16(float a, float b) {  // nearest ev
 // turns them into such columns with byte permutations: no pass through LDS.
 struct Fp8 {
   static constexpr int kBytes = 1;
+  static constexpr int kFoldAhead = 8;  // parts of a tile that are requested at a time: as many as the registers hold
   template <int D> static constexpr int kLoads = D / 64;  // 16-byte loads of a key row per lane
   __device__ static __forceinline__ int dim(int f, int quad) { return 64 * (f >> 1) + 16 * quad + 8 * (f & 1); }
   __device__ static __forceinline__ int load_dim(int j, int quad) { return 64 * j + 16 * quad; }
@@ -255,6 +256,7 @@ struct Fp8 {
 };
 struct Bf16 {
   static constexpr int kBytes = 2;
+  static constexpr int kFoldAhead = 4;
   template <int D> static constexpr int kLoads = D / 32;
   __device__ static __forceinline__ int dim(int f, int quad) { return 32 * f + 8 * quad; }
   __device__ static __forceinline__ int load_dim(int j, int quad) { return 32 * j + 8 * quad; }
@@ -442,7 +444,86 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-constexpr size_t rows_static_lds(int dim) { return 4 * kStaged * 4 + (size_t)kWaves * kRows * (dim + 2) * 4 + 8; }
+constexpr size_t rows_static_lds(int dim) { return 4 * kStaged * 4 + (size_t)kWaves * kRows * (dim + 2) * 4 + 12; }
+
+// Parts of a tile travel between workgroups of one kernel that may run on different dies, whose L2 caches don't see each other: they are
+// written and read as relaxed atomics of device scope, which go through to memory.  (Plain stores with a release fence, which
+// writes back the whole L2, and an acquire fence cost 9 us on a call of 12 and 18 on one of 60.)
+__device__ __forceinline__ void store_part(float* p, float x) { __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ float2 load_part2(const float* p) {  // 8-byte aligned
+  const unsigned long long u = __hip_atomic_load(reinterpret_cast<const unsigned long long*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return make_float2(__uint_as_float((unsigned)u), __uint_as_float((unsigned)(u >> 32)));
+}
+
+// Folds `n` parts of rows row0 .. row1 - 1 of a tile, in one pass over them with a running maximum: D / 4 lanes per row, and as many lanes groups per row (`side`)
+// as the workgroup has, whose results meet in LDS.  part(i): where the i-th
+// lies.  AHEAD of them are requested at a time. 
+template <int D, int AHEAD, class PartFn>
+__device__ __forceinline__ void fold_parts(const Geometry& g, const Seq& s, int tile, int h, int row0, int row1, int n, PartFn part, void* out, f32x4_t* red_o /* [256] */,
+                                           float2* red_ml /* [256 * 4 / D] */) {
+  constexpr int kLanes = D / 4, kGroups = 256 / kLanes, kAhead = AHEAD;
+  const int rows = g.R * g.G;
+  int sides = kGroups;  // a power of two with sides * rows <= kGroups, if there is one
+  while (sides > 1 && sides * (row1 - row0) > kGroups) sides >>= 1;
+  const int at = threadIdx.x % kLanes, group = threadIdx.x / kLanes, side = group & (sides - 1), at_once = kGroups / sides;
+  for (int r0 = row0; r0 < row1; r0 += at_once) {
+    const int r = r0 + group / sides, qr = tile * g.R + r / g.G;
+    const bool live = r < row1 && qr < s.nq;
+    f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+    float m = kNegBig, l = 0.0f;
+    if (live) {
+      for (int i = side; i < n; i += kAhead * sides) {
+        float2 ml[kAhead];
+        f32x4_t x[kAhead];
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) {  // past the end the last part is read again and left out
+          const float* p = part(min(i + e * sides, n - 1));
+          ml[e] = load_part2(p + rows * D + 2 * r);
+          const float2 x0 = load_part2(p + r * D + 4 * at), x1 = load_part2(p + r * D + 4 * at + 2);
+          x[e] = f32x4_t{x0.x, x0.y, x1.x, x1.y};
+          if (i + e * sides >= n) ml[e] = make_float2(-INFINITY, 0.0f);
+        }
+        float mnew = m;
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) mnew = fmaxf(mnew, ml[e].x);
+        const float corr = __builtin_amdgcn_exp2f(m - mnew);
+        m = mnew;
+        l *= corr;
+        o *= corr;
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) {
+          const float f = __builtin_amdgcn_exp2f(ml[e].x - m);
+          l += f * ml[e].y;
+          o += f * x[e];
+        }
+      }
+    }
+    if (sides > 1) {
+      __syncthreads();  // the rows before have been read
+      red_o[threadIdx.x] = o;
+      if (at == 0) red_ml[group] = make_float2(m, l);
+      __syncthreads();
+      if (side == 0) {
+        for (int e = 1; e < sides; ++e) m = fmaxf(m, red_ml[group + e].x);
+        l = 0.0f;
+        o = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int e = 0; e < sides; ++e) {
+          const float f = __builtin_amdgcn_exp2f(red_ml[group + e].x - m);
+          l += f * red_ml[group + e].y;
+          o += f * red_o[threadIdx.x + e * kLanes];
+        }
+      }
+    }
+    if (side == 0 && live) {
+      const size_t a = ((size_t)(s.first + qr) * g.Hq + (size_t)h * g.G + r % g.G) * D + 4 * at;
+      o *= l > 0.0f ? 1.0f / l : 0.0f;
+      if (g.out_bf16)
+        *reinterpret_cast<u32x2_t*>(static_cast<bf16_t*>(out) + a) = u32x2_t{pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};
+      else
+        *reinterpret_cast<f32x4_t*>(static_cast<float*>(out) + a) = o;
+    }
+  }
+}
 
 // A stretch of a tile: as much of a worker's part of it as has its pages in LDS at a time.
 struct Stretch {
@@ -466,6 +547,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(Geometry g, Cache c, 
   __shared__ float red_o[kWaves][kRows][D];
   __shared__ float red_m[kWaves][kRows], red_l[kWaves][kRows];
   __shared__ int missing[2];  // a page of the stretch is not there
+  __shared__ int last_part;
   constexpr int kPer = kStaged / 256;
   constexpr bool kScaled = C::kBytes == 1;
   const int lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
@@ -657,7 +739,9 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(Geometry g, Cache c, 
 #pragma unroll
         for (int n = 0; n < D / 16; ++n) red_o[wave][col][D / 16 * (4 * quad + i) + n] = a.o[n][i];
       lds_barrier();
-      float* po = partials + ((size_t)(2 * worker + (now.begins ? 1 : 0)) * g.Hkv + h) * partial_floats(rows, D);
+      const bool whole = now.begins && now.ends;
+      const size_t one = partial_floats(rows, D);
+      float* po = partials + ((size_t)(2 * worker + (now.begins ? 1 : 0)) * g.Hkv + h) * one;
       for (int i = threadIdx.x; i < rows * D; i += 256) {
         const int r = i / D, d = i % D;
         float m = red_m[0][r], sum = 0.0f, o = 0.0f;
@@ -669,15 +753,35 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(Geometry g, Cache c, 
           sum += f * red_l[w][r];
           o += f * red_o[w][r][d];
         }
-        if (!now.begins || !now.ends) {
-          po[i] = o;
+        if (!whole) {
+          store_part(po + i, o);
           if (d == 0) {
-            po[rows * D + 2 * r] = m;
-            po[rows * D + 2 * r + 1] = sum;
+            store_part(po + rows * D + 2 * r, m);
+            store_part(po + rows * D + 2 * r + 1, sum);
           }
         } else {
           const int qr = now.t.tile * g.R + r / g.G;
           if (qr < now.t.s.nq) store_out(g, out, ((size_t)(now.t.s.first + qr) * g.Hq + (size_t)h * g.G + r % g.G) * D + d, sum > 0.0f ? o / sum : 0.0f);
+        }
+      }
+      if (!whole && c.counters) {
+        // The last of the tile's workgroups to come here folds all parts: every wave's stores have reached memory before it meets the
+        // barrier in front of the count, and what is read behind the count is read from there.
+        const int w1 = (now.t.at + kTileCost) / share + 1;  // the first border inside the tile
+        const int parts = (now.t.at + now.t.units - 1) / share - w1 + 2;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (threadIdx.x == 0) {
+          unsigned* count = c.counters + (size_t)w1 * g.Hkv + h;
+          last_part = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)(parts - 1);
+          if (last_part) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        __syncthreads();
+        if (last_part) {
+          fold_parts<D, C::kFoldAhead>(g, now.t.s, now.t.tile, h, 0, rows, parts,
+                        [&](int i) { return partials + ((size_t)(2 * (w1 - 1 + i) + (i == 0 ? 1 : 0)) * g.Hkv + h) * one; }, out,
+                        reinterpret_cast<f32x4_t*>(&red_o[0][0][0]), reinterpret_cast<float2*>(&red_m[0][0]));
+          __syncthreads();
         }
       }
     }
@@ -686,99 +790,20 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(Geometry g, Cache c, 
   }
 }
 
-// Folds the parts of a tile in one pass: D / 4 lanes per row and part, PARTS parts of the splits of a row side by side (eight where
-// a tile is cut into many splits, one where it has many rows and few splits), each with a running maximum.
-template <int D, bool ROWS, int PARTS>
-__global__ __launch_bounds__(256) void attn_merge_kernel(Geometry g, const int* __restrict__ lengths, const int* __restrict__ offsets, int listed,
-                                                         const float* __restrict__ partials, void* __restrict__ out) {
-  constexpr int kLanes = D / 4, kGroups = 256 / kLanes, kAtOnce = kGroups / PARTS;
-  __shared__ f32x4_t red_o[kGroups][kLanes];
-  __shared__ float2 red_ml[kGroups];
-  const int h = blockIdx.y;
-  Item it;
-  if constexpr (ROWS) {
-    // the first border inside a tile stands for it: its parts are those of the worker in front and of all that begin inside it
-    const int w = blockIdx.x + 1;
-    int total, share;
-    const Border e = border_of(g, lengths, offsets, listed, w, total, share);
-    if (e.b >= g.B || e.unit == 0) return;
-    if ((w - 1) * share > e.at + kTileCost) return;  // not the first
-    it.b = e.b;
-    it.tile = e.tile;
-    it.slot = w - 1;
-    it.n_split = (e.at + e.units - 1) / share - (w - 1) + 1;
-    it.s = e.s;
-  } else {
-    it = find_item<true>(g, lengths, offsets, blockIdx.x);
-    if (it.b < 0) return;
-  }
-  const int rows = g.R * g.G;
-  const size_t one = partial_floats(rows, D), stride = (size_t)g.Hkv * one;
-  const float* base = partials + ((size_t)it.slot * g.Hkv + h) * one;
-  auto part_at = [&](int i) {  // ROWS: place 2 w + 1 of the worker that begins the tile, 2 w of those that go on
-    return ROWS ? partials + ((size_t)(2 * (it.slot + i) + (i == 0 ? 1 : 0)) * g.Hkv + h) * one : base + (size_t)i * stride;
-  };
-  const int at = threadIdx.x % kLanes, group = threadIdx.x / kLanes, part = group % PARTS;
-  for (int r0 = blockIdx.z * kAtOnce; r0 < rows; r0 += gridDim.z * kAtOnce) {
-    const int r = r0 + group / PARTS;
-    const int qr = it.tile * g.R + r / g.G;
-    f32x4_t o = {0.f, 0.f, 0.f, 0.f};
-    float m = kNegBig, l = 0.0f;
-    if (r < rows && qr < it.s.nq) {
-      constexpr int kAhead = 8;
-      for (int i = part; i < it.n_split; i += kAhead * PARTS) {
-        float2 ml[kAhead];
-        f32x4_t x[kAhead];
-#pragma unroll
-        for (int e = 0; e < kAhead; ++e) {  // past the end the last split is read again and left out
-          const float* p = part_at(min(i + e * PARTS, it.n_split - 1));
-          ml[e] = *reinterpret_cast<const float2*>(p + rows * D + 2 * r);
-          x[e] = *reinterpret_cast<const f32x4_t*>(p + r * D + 4 * at);
-          if (i + e * PARTS >= it.n_split) ml[e] = make_float2(-INFINITY, 0.0f);
-        }
-        float mnew = m;
-#pragma unroll
-        for (int e = 0; e < kAhead; ++e) mnew = fmaxf(mnew, ml[e].x);
-        const float corr = __builtin_amdgcn_exp2f(m - mnew);
-        m = mnew;
-        l *= corr;
-        o *= corr;
-#pragma unroll
-        for (int e = 0; e < kAhead; ++e) {
-          const float f = __builtin_amdgcn_exp2f(ml[e].x - m);
-          l += f * ml[e].y;
-          o += f * x[e];
-        }
-      }
-    }
-    if constexpr (PARTS > 1) {
-      __syncthreads();  // the rows before have been read
-      red_o[group][at] = o;
-      if (at == 0) red_ml[group] = make_float2(m, l);
-      __syncthreads();
-      if (part == 0) {
-#pragma unroll
-        for (int e = 1; e < PARTS; ++e) m = fmaxf(m, red_ml[group + e].x);
-        l = 0.0f;
-        o = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int e = 0; e < PARTS; ++e) {
-          const float f = __builtin_amdgcn_exp2f(red_ml[group + e].x - m);
-          l += f * red_ml[group + e].y;
-          o += f * red_o[group + e][at];
-        }
-      }
-    }
-    if (part == 0 && r < rows && qr < it.s.nq) {
-      const size_t a = ((size_t)(it.s.first + qr) * g.Hq + (size_t)h * g.G + r % g.G) * D + 4 * at;
-      const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-      o *= inv;
-      if (g.out_bf16)
-        *reinterpret_cast<u32x2_t*>(static_cast<bf16_t*>(out) + a) = u32x2_t{pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};
-      else
-        *reinterpret_cast<f32x4_t*>(static_cast<float*>(out) + a) = o;
-    }
-  }
+// The parts of tiles of the kernel of 16 rows where that does not fold them itself: one workgroup per (border between workers, head, row).  The first
+// border inside a tile stands for it.
+template <class C, int D>
+__global__ __launch_bounds__(256) void attn_fold_kernel(Geometry g, const int* __restrict__ lengths, const int* __restrict__ offsets, int listed,
+                                                        const float* __restrict__ partials, void* __restrict__ out) {
+  __shared__ f32x4_t red_o[256];
+  __shared__ float2 red_ml[256 * 4 / D];
+  const int w = blockIdx.x + 1, h = blockIdx.y;
+  int total, share;
+  const Border e = border_of(g, lengths, offsets, listed, w, total, share);
+  if (e.b >= g.B || e.unit == 0 || (w - 1) * share > e.at + kTileCost) return;
+  const size_t one = partial_floats(g.R * g.G, D);
+  fold_parts<D, C::kFoldAhead>(g, e.s, e.tile, h, blockIdx.z, blockIdx.z + 1, (e.at + e.units - 1) / share - w + 2,
+                [&](int i) { return partials + ((size_t)(2 * (w - 1 + i) + (i == 0 ? 1 : 0)) * g.Hkv + h) * one; }, out, red_o, red_ml);
 }
 
 // ------------------------------------------------------------------ many queries
@@ -886,6 +911,40 @@ struct BlockStage {
   }
 };
 
+// Folds the splits of the tiles of the kernel below: many rows, few splits.
+template <int D>
+__global__ __launch_bounds__(256) void attn_block_fold_kernel(Geometry g, const int* __restrict__ lengths, const int* __restrict__ offsets,
+                                                              const float* __restrict__ partials, void* __restrict__ out) {
+  constexpr int kLanes = D / 4, kAtOnce = 256 / kLanes;
+  const int h = blockIdx.y, rows = g.R * g.G, at = threadIdx.x % kLanes;
+  const Item it = find_item(g, lengths, offsets, blockIdx.x, true);
+  if (it.b < 0) return;
+  const size_t one = partial_floats(rows, D), stride = (size_t)g.Hkv * one;
+  const float* base = partials + (size_t)it.slot * stride + h * one;
+  for (int r = blockIdx.z * kAtOnce + threadIdx.x / kLanes; r < rows; r += gridDim.z * kAtOnce) {
+    const int qr = it.tile * g.R + r / g.G;
+    if (qr >= it.s.nq) return;
+    float m = kNegBig, l = 0.0f;
+    f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int i = 0; i < it.n_split; ++i) {
+      const float* p = base + i * stride;
+      const float2 ml = *reinterpret_cast<const float2*>(p + rows * D + 2 * r);
+      const f32x4_t x = *reinterpret_cast<const f32x4_t*>(p + r * D + 4 * at);
+      const float mnew = fmaxf(m, ml.x), corr = __builtin_amdgcn_exp2f(m - mnew), f = __builtin_amdgcn_exp2f(ml.x - mnew);
+      m = mnew;
+      l = l * corr + f * ml.y;
+      o = o * corr + f * x;
+    }
+    const size_t a = ((size_t)(it.s.first + qr) * g.Hq + (size_t)h * g.G + r % g.G) * D + 4 * at;
+    o *= l > 0.0f ? 1.0f / l : 0.0f;
+    if (g.out_bf16)
+      *reinterpret_cast<u32x2_t*>(static_cast<bf16_t*>(out) + a) = u32x2_t{pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};
+    else
+      *reinterpret_cast<f32x4_t*>(static_cast<float*>(out) + a) = o;
+  }
+}
+
 // TERMS: bf16 terms of a weight: one where the output is bf16 (2^-9 of a weight, no more than the output's own rounding), three
 // for an fp32 output.
 template <class C, int D, int TERMS>
@@ -896,7 +955,7 @@ __global__ __launch_bounds__(256, 2) void attn_block_kernel(Geometry g, Cache c,
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // the heads of a KV head's tokens follow each other, so that with eight of them an XCD's L2 holds the rows of one
   const int item = blockIdx.x / g.Hkv, h = blockIdx.x - item * g.Hkv;
-  const Item it = find_item<false>(g, c.lengths, offsets, item);
+  const Item it = find_item(g, c.lengths, offsets, item, false);
   if (it.b < 0) return;
   const int r = 32 * wave + col, qi = it.tile * g.R + r / g.G;
   const bool row_ok = r < g.R * g.G && qi < it.s.nq;

@@ -25,7 +25,7 @@ class Config(C.Structure):
 
 
 class Pages(C.Structure):
-    _fields_ = [(n, C.c_void_p) for n in ("k_pages", "v_pages", "k_scale", "v_scale", "page_table", "lengths")]
+    _fields_ = [(n, C.c_void_p) for n in ("k_pages", "v_pages", "k_scale", "v_scale", "page_table", "lengths", "counters")]
 
 
 _lib = None
@@ -38,6 +38,8 @@ def _load():
         vp, cfg, pages, i32, i64, size = C.c_void_p, C.POINTER(Config), C.POINTER(Pages), C.c_int32, C.c_int64, C.c_size_t
         lib.pqc_paged_append.restype = C.c_int
         lib.pqc_paged_append.argtypes = [cfg, pages, vp, i64, vp, i64, vp, i64, i32, vp, vp, vp, vp, vp, vp]
+        lib.pqc_paged_counter_bytes.restype = size
+        lib.pqc_paged_counter_bytes.argtypes = [cfg]
         lib.pqc_paged_workspace_bytes.restype = size
         lib.pqc_paged_workspace_bytes.argtypes = [cfg, i32, i32]
         lib.pqc_paged_attn.restype = C.c_int
@@ -88,10 +90,13 @@ class PagedCache:
         self.cfg = Config(1, n_q_heads, heads, dim, tokens, n_pages, 1, _DTYPES[dtype][0], 2 if fp8 else 1, _DTYPES[out_dtype][0],
                           softmax_scale, rot_dims, _STYLES[rot_style], rot_positions)
         self.pages = Pages(k_pages.data_ptr(), v_pages.data_ptr(), k_scale.data_ptr() if fp8 else None,
-                           v_scale.data_ptr() if fp8 else None, None, None)
+                           v_scale.data_ptr() if fp8 else None, None, None, None)
         self._cfg, self._pages = C.byref(self.cfg), C.byref(self.pages)
         self._dev = k_pages.get_device()
         self._sizes = {}  # workspace bytes by (batch, listed tokens)
+        # counters (pqc_paged_counter_bytes): one block per stream, and one of its own for each recorded call, so that neither two
+        # streams nor two graphs share any; without a block a call takes two launches
+        self._counters, self._spare, self._recorded = {}, [], []
 
     @classmethod
     def empty(cls, n_pages: int, n_q_heads: int, n_kv_heads: int, head_dim: int = 128, page_tokens: int = 64, cache_dtype: str = "fp8",
@@ -171,6 +176,31 @@ class PagedCache:
             ws.record_stream(stream)  # not given to another tensor before the call has run there
         return ws, ws.data_ptr()
 
+    def _count_on(self, stream) -> None:
+        """Sets the counters of an attention call on `stream` (None: the current one)."""
+        if self._dev < 0:
+            return
+        if stream is not None and stream.cuda_stream != torch._C._cuda_getCurrentRawStream(self._dev):
+            with torch.cuda.stream(stream):
+                return self._count_on(None)
+        if torch._C._cuda_isCurrentStreamCapturing():
+            if self._spare:
+                self._recorded.append(self._spare.pop())
+                self.pages.counters = self._recorded[-1].data_ptr()
+            else:
+                self.pages.counters = None
+            return
+        st = torch._C._cuda_getCurrentRawStream(self._dev)
+        block = self._counters.get(st)
+        if block is None:
+            words = self.lib.pqc_paged_counter_bytes(self._cfg) // 4
+            fill = not self._counters
+            blocks = torch.zeros((33 if fill else 1, max(words, 1)), dtype=torch.int32, device=self.device)
+            block = self._counters[st] = blocks[0]
+            if fill:
+                self._spare = list(blocks[1:])
+        self.pages.counters = block.data_ptr()
+
     # -- entry points (same names as the C ABI)
     def append(self, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor, *, new_offsets=None, q=None,
                positions=None, q_out=None, k_out=None, stream=None):
@@ -204,6 +234,7 @@ class PagedCache:
             out = torch.empty((n, self.q_heads, self.dim), dtype=self.out, device=self.device)
         op = self._plain(out, self.out, n, self.q_heads, "out")
         if n:
+            self._count_on(stream)
             ws, wp = self._workspace(self.cfg.batch, 0, stream)
             self._call("pqc_paged_attn", self.lib.pqc_paged_attn, stream, (self._cfg, self._pages, qp, n, off, op, wp, 0 if ws is None else ws.numel()))
         return out
@@ -219,6 +250,7 @@ class PagedCache:
         if out is None:
             out = torch.empty((b, self.q_heads, self.dim), dtype=self.out, device=self.device)
         op = self._plain(out, self.out, b, self.q_heads, "out")
+        self._count_on(stream)
         ws, wp = self._workspace(b, n_idx, stream)
         self._call("pqc_paged_gather_attn", self.lib.pqc_paged_gather_attn, stream,
                    (self._cfg, self._pages, qp, idx.data_ptr(), n_idx, op, wp, 0 if ws is None else ws.numel()))

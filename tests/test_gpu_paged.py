@@ -420,6 +420,44 @@ def test_a_recorded_step_follows_its_tables_and_lengths(paged):
                 assert torch.equal(a[row[p], :, :n].view(torch.uint8), b[row[p], :, :n].view(torch.uint8))
 
 
+@pytest.mark.parametrize("lengths,P,heads,G,D,cache,dtype", [
+    ([20011] * 5, 16, 8, 4, 128, "fp8", "bf16"), ([9000] + [3] * 70, 64, 2, 1, 64, "fp8", "bf16"), ([2048], 64, 8, 4, 128, "fp8", "bf16"),
+    ([1500, 0, 1300, 1], 32, 2, 16, 128, "bf16", "f32"), ([1900, 700], 128, 3, 3, 64, "bf16", "bf16"), ([2000, 1300, 700, 1], 64, 8, 8, 128, "fp8", "f32")])
+def test_parts_folded_by_the_last_workgroup_or_by_a_kernel(paged, lengths, P, heads, G, D, cache, dtype):
+    # either way within the tolerance, the same from call to call, and a call leaves its counters zero
+    gen = torch.Generator().manual_seed(P + G)
+    c, pages, table = make(paged, gen, lengths, P, heads, G, D, cache, dtype, "f32")
+    B = len(lengths)
+    q = torch.randn((B, heads * G, D), generator=gen).to(IO[dtype])
+    idx = torch.randint(0, max(lengths), (B, heads, 2000), generator=gen).int()
+    dq, di, dt, lens = dev(q), dev(idx), dev(table), dev(torch.tensor(lengths, dtype=torch.int32))
+    last = [c.attn(dq, dt, lens) for _ in range(3)] + [c.gather_attn(dq, di, dt, lens) for _ in range(3)]
+    torch.cuda.synchronize()
+    blocks = list(c._counters.values())
+    assert len(blocks) == 1 and not bool(blocks[0].any())
+    c._count_on = lambda stream: setattr(c.pages, "counters", None)
+    own = [c.attn(dq, dt, lens) for _ in range(3)] + [c.gather_attn(dq, di, dt, lens) for _ in range(3)]
+    torch.cuda.synchronize()
+    few = [b for b in range(B) if lengths[b] < 5000][:3] + [0]
+    for res in (last, own):
+        for i, listed in ((0, None), (3, idx)):
+            assert torch.equal(res[i], res[i + 1]) and torch.equal(res[i], res[i + 2])
+            for b in few:
+                want, tol = ref.attention(q[b:b + 1], pages, table[b:b + 1], torch.tensor(lengths[b:b + 1]), None, D ** -0.5, "f32",
+                                          listed=None if listed is None else listed[b:b + 1])
+                close(res[i][b:b + 1], want, tol, f"{i} {b}")
+
+
+def test_launches_of_a_step(paged):
+    from parity_utils import count_launches
+
+    c, _, table = make(paged, torch.Generator().manual_seed(1), [3000] * 5, 64, 8, 4, 128, "fp8", "bf16", "f32")
+    q, table, lens = torch.zeros((5, 32, 128), dtype=torch.bfloat16, device=DEV), dev(table), torch.tensor([3000] * 5, dtype=torch.int32, device=DEV)
+    assert count_launches(lambda: c.attn(q, table, lens)) == 1
+    c._spare.clear()
+    assert count_launches(lambda: c.attn(q, table, lens)) == 2
+
+
 def test_retrieval_over_a_paged_cache(paged):
     """A prompt, PQ structures of its rotated keys, then steps of generation: append, code of the new token, table, scan, top-k and
     attention to the selected tokens of the 8-bit cache; against 64 bits on the values that the cache stands for."""
