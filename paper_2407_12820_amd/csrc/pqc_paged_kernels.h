@@ -111,6 +111,7 @@ __device__ __forceinline__ Item find_item(const Geometry& g, const int* lengths,
       const int nth = whole_tiles ? at : at / it.n_split;
       it.tile = __builtin_amdgcn_readlane(tiles, l) - 1 - nth;  // the last one, which sees most, first
       it.split = whole_tiles ? 0 : at - nth * it.n_split;
+      if (it.n_split > 1) it.tokens = ((__builtin_amdgcn_readlane(s.len, l) + it.n_split - 1) / it.n_split + kGrain - 1) / kGrain * kGrain;  // equal splits
       it.slot = it.n_split > 1 ? slots + __builtin_amdgcn_readlane(slot_end - mine, l) + nth * it.n_split : -1;
       it.s.first = __builtin_amdgcn_readlane(s.first, l);
       it.s.nq = __builtin_amdgcn_readlane(s.nq, l);
@@ -818,51 +819,65 @@ __global__ __launch_bounds__(256) void attn_fold_kernel(Geometry g, const int* _
 // computed, the page of those behind them one round earlier.
 typedef __attribute__((ext_vector_type(16))) float f32x16_t;
 
+// Keys of 64 tokens and values of 64 others on their way from the pages to LDS.  A wave brings 16 of either, which lie in one page, so
+// that pages, scales and addresses are scalar.
 template <class C, int D>
 struct BlockStage {
-  static constexpr int kK = D / 64 * C::kBytes;           // 16-byte loads of keys per thread: token tid / 4
-  static constexpr int kV = C::kBytes;                    // words of each of eight tokens' values: four dimensions
-  static constexpr bool kHalfV = D == 64;                 // half of the threads stage values
+  static constexpr int kK = D / 64 * C::kBytes;   // 16-byte loads of keys per thread: token tid / 4
+  static constexpr int kV = C::kBytes;            // words of each of eight tokens' values: four dimensions
+  static constexpr int kVLanes = D / 2;           // lanes of a wave that bring values
   u32x4_t k[kK];
   unsigned v[8][kV];
   float ks, vs;
   bool k_ok, v_ok;
-  int token;  // the first of the 64
+  int vzero;  // 0 in a vector register: pages and scales come by vector loads, which keep their order.  A scalar load that misses is
+              // what every wait for LDS behind it waits for too.
 
-  // pages of the thread's key token and of its eight value tokens
-  __device__ __forceinline__ void load(const Geometry& g, const Cache& c, int h, int t, int k_page, int v_page) {
-    const int tid = threadIdx.x;
-    token = t;
-    k_ok = k_page >= 0;
-    v_ok = v_page >= 0;
-    const size_t kp = (size_t)max(k_page, 0) * g.Hkv + h, vp = (size_t)max(v_page, 0) * g.Hkv + h;
-    ks = vs = 1.0f;
-    if constexpr (C::kBytes == 1) {
-      if (k_ok) ks = c.ks[kp];
-      if (v_ok) vs = c.vs[vp];
-    }
-    const unsigned char* kr = c.k + ((kp << g.shift) + ((t + tid / 4) & (g.P - 1))) * (size_t)(D * C::kBytes);
-    const int q = tid & 3;
+  // `t`: the wave's first token, `page`: its page, negative if there is none
+  __device__ __forceinline__ void load_k(const Geometry& g, const Cache& c, int h, int t, int page) {
+    const int lane = threadIdx.x & 63, q = lane & 3;
+    k_ok = page >= 0;
+    const size_t p = (size_t)max(page, 0) * g.Hkv + h;
+    ks = C::kBytes == 1 ? c.ks[p + vzero] : 1.0f;
+    const unsigned char* kr = c.k + ((p << g.shift) + (t & (g.P - 1))) * (size_t)(D * C::kBytes);
 #pragma unroll
     for (int j = 0; j < kK; ++j) {
       const int dim = C::kBytes == 1 ? 64 * j + 16 * q : 64 * (j >> 1) + 16 * q + 8 * (j & 1);
-      k[j] = *reinterpret_cast<const u32x4_t*>(kr + dim * C::kBytes);
-    }
-    if (!kHalfV || tid < 128) {
-      const int chunk = tid / (D / 4), dg = tid % (D / 4);
-      const unsigned char* vr = c.v + ((vp << g.shift) + ((t + 16 * (chunk >> 1) + 4 * (chunk & 1)) & (g.P - 1))) * (size_t)(D * C::kBytes) + dg * 4 * C::kBytes;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) load_words(vr + (e < 4 ? e : e + 4) * (D * C::kBytes), v[e]);
+      k[j] = *reinterpret_cast<const u32x4_t*>(kr + (unsigned)((lane / 4 * D + dim) * C::kBytes));
     }
   }
-  // tokens from `most` on are zero, and those of pages that are not there
-  __device__ __forceinline__ void store(unsigned char* lk, unsigned char* lv, int most) {
-    const int tid = threadIdx.x, row = tid / 4, q = tid & 3;
-    if (!k_ok || token + row >= most) {
+  __device__ __forceinline__ void load_v(const Geometry& g, const Cache& c, int h, int t, int page) {
+    const int lane = threadIdx.x & 63;
+    v_ok = page >= 0;
+    const size_t p = (size_t)max(page, 0) * g.Hkv + h;
+    vs = C::kBytes == 1 ? c.vs[p + vzero] : 1.0f;
+    if (lane < kVLanes) {
+      const unsigned char* vr = c.v + ((p << g.shift) + (t & (g.P - 1))) * (size_t)(D * C::kBytes);
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        load_words(vr + (unsigned)(((4 * (lane / (D / 4)) + (e < 4 ? e : e + 4)) * D + lane % (D / 4) * 4) * C::kBytes), v[e]);
+    }
+  }
+  // Tokens from `most` on are zero, and those of pages that are not there: their rows may hold anything.
+  __device__ __forceinline__ void clear_k(int t, int most) {
+    if (!k_ok || t + (int)(threadIdx.x & 63) / 4 >= most) {
 #pragma unroll
       for (int j = 0; j < kK; ++j) k[j] = u32x4_t{0u, 0u, 0u, 0u};
-      ks = 1.0f;
     }
+    if (!k_ok) ks = 1.0f;
+  }
+  __device__ __forceinline__ void clear_v(int t, int most) {
+    const int first = t + 4 * ((threadIdx.x & 63) / (D / 4));
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (!v_ok || first + (e < 4 ? e : e + 4) >= most) {
+#pragma unroll
+        for (int i = 0; i < kV; ++i) v[e][i] = 0u;
+      }
+    if (!v_ok) vs = 1.0f;
+  }
+  __device__ __forceinline__ void store_k(unsigned char* lk) const {
+    const int tid = threadIdx.x, row = tid / 4, q = tid & 3;
     unsigned char* kr = lk + row * (D * 2);
 #pragma unroll
     for (int j = 0; j < D / 64; ++j)
@@ -875,38 +890,30 @@ struct BlockStage {
           w = k[2 * j + e];
         *reinterpret_cast<u32x4_t*>(kr + (((8 * j + 2 * q + e) ^ (row & 7)) << 4)) = w;
       }
-    if (!kHalfV || tid < 128) {
-      const int chunk = tid / (D / 4), dg = tid % (D / 4);
-      const int first = token + 16 * (chunk >> 1) + 4 * (chunk & 1);
-      if (!v_ok || first + 12 > most) {
+  }
+  __device__ __forceinline__ void store_v(unsigned char* lv, int wave) const {
+    const int lane = threadIdx.x & 63;
+    if (lane >= kVLanes) return;
+    const int chunk = 2 * wave + lane / (D / 4), dg = lane % (D / 4);
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (!v_ok || first + (e < 4 ? e : e + 4) >= most) {
+    for (int j = 0; j < 2; ++j) {
+      u32x4_t even, odd;
 #pragma unroll
-            for (int i = 0; i < kV; ++i) v[e][i] = 0u;
-          }
-        if (!v_ok) vs = 1.0f;
-      }
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        u32x4_t even, odd;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          unsigned a, b;
-          if constexpr (C::kBytes == 1) {
-            a = C::two(v[2 * e][0], j == 1, vs);
-            b = C::two(v[2 * e + 1][0], j == 1, vs);
-          } else {
-            a = v[2 * e][j];
-            b = v[2 * e + 1][j];
-          }
-          even[e] = __builtin_amdgcn_perm(b, a, 0x05040100u);
-          odd[e] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+      for (int e = 0; e < 4; ++e) {
+        unsigned a, b;
+        if constexpr (C::kBytes == 1) {
+          a = C::two(v[2 * e][0], j == 1, vs);
+          b = C::two(v[2 * e + 1][0], j == 1, vs);
+        } else {
+          a = v[2 * e][j];
+          b = v[2 * e + 1][j];
         }
-        const int d = 4 * dg + 2 * j;
-        *reinterpret_cast<u32x4_t*>(lv + d * 128 + ((chunk ^ ((d ^ (d >> 2)) & 7)) << 4)) = even;
-        *reinterpret_cast<u32x4_t*>(lv + (d + 1) * 128 + ((chunk ^ (((d + 1) ^ ((d + 1) >> 2)) & 7)) << 4)) = odd;
+        even[e] = __builtin_amdgcn_perm(b, a, 0x05040100u);
+        odd[e] = __builtin_amdgcn_perm(b, a, 0x07060302u);
       }
+      const int d = 4 * dg + 2 * j;
+      *reinterpret_cast<u32x4_t*>(lv + d * 128 + ((chunk ^ ((d ^ (d >> 2)) & 7)) << 4)) = even;
+      *reinterpret_cast<u32x4_t*>(lv + (d + 1) * 128 + ((chunk ^ (((d + 1) ^ ((d + 1) >> 2)) & 7)) << 4)) = odd;
     }
   }
 };
@@ -947,11 +954,17 @@ __global__ __launch_bounds__(256) void attn_block_fold_kernel(Geometry g, const 
 
 // TERMS: bf16 terms of a weight: one where the output is bf16 (2^-9 of a weight, no more than the output's own rounding), three
 // for an fp32 output.
+// The vector ALU has about as much to do as the matrix cores (64 tokens, one wave: 32 exponentials and some 200 other instructions,
+// 1000 to 1300 cycles, against 32 matrix instructions of 32), so the two run side by side within a wave: the weights of a round's tokens
+// are computed while the values of the round before are multiplied, keys being a round ahead of values.  Two workgroups share a compute
+// unit (one alone takes 1.4 times as long).  Prompts of 8192 tokens, 32 query heads, 8 KV heads: 590 us, 930 TFLOP/s; round after
+// round without the overlap 634; operands read one instruction ahead instead of four 604.  64 rows per wave, which would halve the
+// reads of LDS, need more registers than the vector ALU reaches and spend the gain on copies.
 template <class C, int D, int TERMS>
 __global__ __launch_bounds__(256, 2) void attn_block_kernel(Geometry g, Cache c, const bf16_t* __restrict__ q, const int* __restrict__ offsets,
                                                             void* __restrict__ out, float* __restrict__ partials) {
   __shared__ __align__(16) unsigned char lds_k[2][kBlockTokens * D * 2], lds_v[2][kBlockTokens * D * 2];
-  __shared__ unsigned present[2];  // a byte per 16 tokens: their page is there
+  __shared__ unsigned present[2];  // a byte per 16 tokens of keys: their page is there
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // the heads of a KV head's tokens follow each other, so that with eight of them an XCD's L2 holds the rows of one
   const int item = blockIdx.x / g.Hkv, h = blockIdx.x - item * g.Hkv;
@@ -984,98 +997,212 @@ __global__ __launch_bounds__(256, 2) void attn_block_kernel(Geometry g, Cache c,
   float m = kNegBig, l = 0.0f;
 
   const int t0 = it.split * it.tokens, t1 = it.n_split == 1 ? most : min(t0 + it.tokens, most);
-  if (t0 < t1) {
+  const int rounds = t0 < t1 ? (t1 - t0 + kBlockTokens - 1) / kBlockTokens : 0;
+  const int mine = min(rounds, max(0, (wave_most - t0 + kBlockTokens - 1) / kBlockTokens));  // that the wave's rows see anything of
+  if (rounds > 0) {
     const int* table = c.table + (size_t)it.b * g.max_pages;
-    const int v_at = 16 * ((tid / (D / 4)) >> 1);  // the thread's value tokens' page (threads without any: some page of the row)
-    auto page_of = [&](int t) {
-      const int p = t < t1 ? table[t >> g.shift] : -1;
+    BlockStage<C, D> st;
+    asm("v_mov_b32 %0, 0" : "=v"(st.vzero));
+    auto page_of = [&](int i) {  // of the wave's tokens of round i
+      const int t = t0 + i * kBlockTokens + 16 * wave;
+      return t < t1 ? table[(t >> g.shift) + st.vzero] : -1;
+    };
+    auto valid = [&](int loaded) {
+      const int p = __builtin_amdgcn_readfirstlane(loaded);
       return p < g.n_pages ? p : -1;
     };
-    BlockStage<C, D> st;
-    auto put = [&](int buf) {
-      st.store(lds_k[buf], lds_v[buf], most);
-      if ((tid & 63) == 0) reinterpret_cast<unsigned char*>(&present[buf])[wave] = (unsigned char)st.k_ok;  // wave: tokens 16 wave .. + 15
+    auto wave_token = [&](int i) { return t0 + i * kBlockTokens + 16 * wave; };
+    auto put_k = [&](int i) {
+      if (!st.k_ok || wave_token(i) + 16 > most) st.clear_k(wave_token(i), most);
+      st.store_k(lds_k[i & 1]);
+      if (lane == 0) reinterpret_cast<unsigned char*>(&present[i & 1])[wave] = (unsigned char)st.k_ok;
     };
-    st.load(g, c, h, t0, page_of(t0 + tid / 4), page_of(t0 + (v_at & 63)));
-    int k_page = page_of(t0 + kBlockTokens + tid / 4), v_page = page_of(t0 + kBlockTokens + (v_at & 63));
-    put(0);
+    auto put_v = [&](int i) {
+      if (!st.v_ok || wave_token(i) + 16 > most) st.clear_v(wave_token(i), most);
+      st.store_v(lds_v[i & 1], wave);
+    };
+    constexpr int kAhead = 4;
+    f32x16_t s[2];
+    unsigned w[TERMS == 1 ? 16 : 32];  // weights of a round: pairs of bf16, or fp32 until they are multiplied
+    // Where the lane reads its operands; the chunk of an instruction is an exclusive or with its number (worked out anew in each
+    // round: sixteen addresses kept in registers leave too few for operands read ahead).
+    unsigned k_at = col * (D * 2) + ((half ^ (col & 7)) << 4), v_at = col * 128 + ((half ^ ((col ^ (col >> 2)) & 7)) << 4);
+    float reference = 0.0f;
+    auto logits = [&](int i) {
+      asm("" : "+v"(k_at));
+      const unsigned char* at = lds_k[i & 1];
+      bf16x8_t k[2 * (D / 16)];
+#pragma unroll
+      for (int e = 0; e < D / 16; ++e)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) __builtin_memcpy(&k[2 * e + b], at + 32 * b * (D * 2) + (k_at ^ (e << 5)), 16);
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[b][e] = 0.0f;
+#pragma unroll
+      for (int e = 0; e < D / 16; ++e)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[2 * e + b], qf[e], s[b], 0, 0, 0);
+      // operands are read kAhead instructions ahead
+#pragma unroll
+      for (int e = 0; e < kAhead; ++e) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+#pragma unroll
+      for (int e = 0; e < 2 * (D / 16) - kAhead; ++e) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
+    };
+    auto mask = [&](int i) {
+      const int t = t0 + i * kBlockTokens;
+      const unsigned there = __builtin_amdgcn_readfirstlane(present[i & 1]);
+      if (t + kBlockTokens > least || there != 0x01010101u) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int at = 32 * b + 8 * (e >> 2) + 4 * half + (e & 3);
+            if (t + at >= lim || !((there >> (8 * (at >> 4))) & 1u)) s[b][e] = -INFINITY;
+          }
+      }
+    };
+    // Exponents of the weights, relative to m (to 0 as long as the row has seen nothing).  Weights may reach 2^8 before a larger
+    // maximum is taken: O and l are relative to the same.
+    auto raise = [&](float& corr) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        s[0][e] = fmaf(s[0][e], g.scale_log2e, -reference);
+        s[1][e] = fmaf(s[1][e], g.scale_log2e, -reference);
+        mx = fmaxf(mx, fmaxf(s[0][e], s[1][e]));
+      }
+      const u32x2_t both = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+      mx = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) + reference;
+      const bool up = __any(mx > m + 8.0f);
+      if (up) {
+        const float mnew = fmaxf(m, mx);
+        corr = __builtin_amdgcn_exp2f(m - mnew);
+        m = mnew;
+        l *= corr;
+        const float ref = m > 0.5f * kNegBig ? m : 0.0f, by = ref - reference;
+        reference = ref;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          s[0][e] -= by;
+          s[1][e] -= by;
+        }
+      }
+      return up;
+    };
+    auto weigh = [&](int b, int k) {  // 16 tokens
+#pragma unroll
+      for (int e = 8 * k; e < 8 * k + 8; e += 2) {
+        const float p0 = __builtin_amdgcn_exp2f(s[b][e]), p1 = __builtin_amdgcn_exp2f(s[b][e + 1]);
+        if constexpr (TERMS == 1) {
+          const unsigned u = w[8 * b + e / 2] = pack_bf16(p0, p1);
+          bf16x2_t p, one = {(__bf16)1.0f, (__bf16)1.0f};
+          __builtin_memcpy(&p, &u, 4);
+          l = __builtin_amdgcn_fdot2_f32_bf16(p, one, l, false);  // the sum of the weights as they are multiplied
+        } else {
+          l += p0 + p1;
+          w[16 * b + e] = __float_as_uint(p0);
+          w[16 * b + e + 1] = __float_as_uint(p1);
+        }
+      }
+    };
+    auto multiply = [&](int i, int b, int k) {
+      bf16x8_t p[TERMS];
+      if constexpr (TERMS == 1) {
+        __builtin_memcpy(&p[0], &w[8 * b + 4 * k], 16);
+      } else {
+        u32x4_t x[TERMS];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float p0 = __uint_as_float(w[16 * b + 8 * k + 2 * e]), p1 = __uint_as_float(w[16 * b + 8 * k + 2 * e + 1]);
+#pragma unroll
+          for (int y = 0; y < TERMS; ++y) {
+            x[y][e] = pack_bf16(p0, p1);
+            p0 -= __uint_as_float(x[y][e] << 16);
+            p1 -= __uint_as_float(x[y][e] & 0xffff0000u);
+          }
+        }
+#pragma unroll
+        for (int y = 0; y < TERMS; ++y) __builtin_memcpy(&p[y], &x[y], 16);
+      }
+#pragma unroll
+      for (int n = 0; n < D / 32; ++n) {
+        bf16x8_t v;
+        __builtin_memcpy(&v, lds_v[i & 1] + 4096 * n + (v_at ^ ((2 * b + k) << 5)), 16);
+#pragma unroll
+        for (int y = 0; y < TERMS; ++y) o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[y], o[n], 0, 0, 0);
+      }
+    };
+
+    // in front of round i LDS holds keys i + 1 and values i, the registers keys i + 2 and values i + 1
+    const int page1 = valid(page_of(1));
+    int page2 = valid(page_of(2)), page3 = page_of(3);
+    {
+      const int page0 = valid(page_of(0));
+      st.load_k(g, c, h, wave_token(0), page0);
+      st.load_v(g, c, h, wave_token(0), page0);
+    }
+    put_k(0);
+    st.load_k(g, c, h, wave_token(1), page1);
     __syncthreads();
-    for (int t = t0, buf = 0; t < t1; t += kBlockTokens, buf ^= 1) {
-      const bool more = t + kBlockTokens < t1;
-      if (more) {
-        st.load(g, c, h, t + kBlockTokens, k_page, v_page);
-        k_page = page_of(t + 2 * kBlockTokens + tid / 4);
-        v_page = page_of(t + 2 * kBlockTokens + (v_at & 63));
+    if (mine > 0) {
+      float corr;
+      logits(0);
+      mask(0);
+      raise(corr);
+#pragma unroll
+      for (int b = 0; b < 4; ++b) weigh(b >> 1, b & 1);
+    }
+    put_k(1);
+    put_v(0);
+    st.load_k(g, c, h, wave_token(2), page2);
+    st.load_v(g, c, h, wave_token(1), page1);
+    auto stage = [&](int i) {
+      put_k(i + 2);
+      put_v(i + 1);
+      const int next = valid(page3);
+      st.load_k(g, c, h, wave_token(i + 3), next);
+      st.load_v(g, c, h, wave_token(i + 2), page2);
+      page2 = next;
+      page3 = page_of(i + 4);
+    };
+    // a larger maximum reaches O one round late, behind the values whose weights were relative to the old one
+    float late = 1.0f;
+    bool up = false;
+    auto rescale = [&]() {
+      if (up) {
+#pragma unroll
+        for (int n = 0; n < D / 32; ++n) o[n] *= late;
       }
-      if (t < wave_most) {
-        f32x16_t s[2];
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) s[b][i] = 0.0f;
-          const int row = 32 * b + col;
-#pragma unroll
-          for (int i = 0; i < D / 16; ++i) {
-            bf16x8_t k;
-            __builtin_memcpy(&k, lds_k[buf] + row * (D * 2) + (((2 * i + half) ^ (row & 7)) << 4), 16);
-            s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, qf[i], s[b], 0, 0, 0);
-          }
-        }
-        const unsigned there = __builtin_amdgcn_readfirstlane(present[buf]);
-        if (t + kBlockTokens > least || there != 0x01010101u) {
-#pragma unroll
-          for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const int at = 32 * b + 8 * (i >> 2) + 4 * half + (i & 3);
-              if (t + at >= lim || !((there >> (8 * (at >> 4))) & 1u)) s[b][i] = -INFINITY;
-            }
-        }
-        float mx = kNegBig;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, fmaxf(s[0][i], s[1][i]));
-        const u32x2_t both = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-        mx = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * g.scale_log2e;
-        // weights may reach 2^8 before a larger maximum is taken: they are relative to it in O and l alike
-        if (__any(mx > m + 8.0f)) {
-          const float mnew = fmaxf(m, mx), corr = __builtin_amdgcn_exp2f(m - mnew);
-          m = mnew;
-          l *= corr;
-#pragma unroll
-          for (int n = 0; n < D / 32; ++n) o[n] *= corr;
-        }
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          unsigned w[TERMS][8];
-#pragma unroll
-          for (int i = 0; i < 16; i += 2) {
-            float p0 = __builtin_amdgcn_exp2f(fmaf(s[b][i], g.scale_log2e, -m)), p1 = __builtin_amdgcn_exp2f(fmaf(s[b][i + 1], g.scale_log2e, -m));
-            l += p0 + p1;
-#pragma unroll
-            for (int e = 0; e < TERMS; ++e) {
-              w[e][i / 2] = pack_bf16(p0, p1);
-              p0 -= __uint_as_float(w[e][i / 2] << 16);
-              p1 -= __uint_as_float(w[e][i / 2] & 0xffff0000u);
-            }
-          }
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            bf16x8_t p[TERMS];
-#pragma unroll
-            for (int e = 0; e < TERMS; ++e) __builtin_memcpy(&p[e], &w[e][4 * k], 16);
-#pragma unroll
-            for (int n = 0; n < D / 32; ++n) {
-              const int d = 32 * n + col;
-              bf16x8_t v;
-              __builtin_memcpy(&v, lds_v[buf] + d * 128 + (((2 * (2 * b + k) + half) ^ ((d ^ (d >> 2)) & 7)) << 4), 16);
-#pragma unroll
-              for (int e = 0; e < TERMS; ++e) o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[e], o[n], 0, 0, 0);
-            }
-          }
-        }
-      }
-      if (more) put(buf ^ 1);
+    };
+    int i = 0;
+    for (; i + 1 < mine; ++i) {
       __syncthreads();
+      logits(i + 1);
+      stage(i);
+      mask(i + 1);
+      rescale();
+      up = raise(late);
+      asm("" : "+v"(v_at));
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        multiply(i, b >> 1, b & 1);
+        weigh(b >> 1, b & 1);
+      }
+    }
+    for (; i < rounds; ++i) {  // the wave's last, and those of other waves
+      __syncthreads();
+      if (i + 1 < rounds) stage(i);
+      if (i < mine) {
+        rescale();
+#pragma unroll
+        for (int b = 0; b < 4; ++b) multiply(i, b >> 1, b & 1);
+      }
     }
   }
   const u32x2_t both = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
@@ -1087,9 +1214,7 @@ __global__ __launch_bounds__(256, 2) void attn_block_kernel(Geometry g, Cache c,
 #pragma unroll
     for (int n = 0; n < D / 32; ++n)
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) po[r * D + 32 * n + 8 * j + 4 * half + i] = o[n][4 * j + i];
+      for (int j = 0; j < 4; ++j) *reinterpret_cast<f32x4_t*>(po + r * D + 32 * n + 8 * j + 4 * half) = f32x4_t{o[n][4 * j], o[n][4 * j + 1], o[n][4 * j + 2], o[n][4 * j + 3]};
     if (half == 0) {
       po[rows * D + 2 * r] = m;
       po[rows * D + 2 * r + 1] = l;
