@@ -19,6 +19,10 @@ bool aligned(const void* p, unsigned n) { return (reinterpret_cast<uintptr_t>(p)
 // sequences of 68224 tokens 233 us, 202 with it).
 constexpr int kWorkers = 512;
 constexpr size_t kRowsLds = 56 * 1024;
+// One per compute unit where there is little to do for each: twice as many have as many more parts to fold.  us with 512 and 256, 8 heads of 4
+// query heads, one sequence of 4096 tokens 13.4, 12.8, 6144 15.6, 13.5, 16384 19.5, 18.0, 32768 23.5, 23.5, two of 4096 17.1, 14.4; listed, 4096
+// tokens 13.0, 12.0, 6600 14.6, 13.1, 13175 16.4, 15.4.
+constexpr int kFewUnits = 4;
 // Items of the kernel of 128 rows that the length of a split aims at.
 constexpr int kBlockItems = 480;
 
@@ -68,6 +72,7 @@ Tiles tiles_for(const pqc_paged_config* c, const Geometry& g, const int* offsets
 // The kernel of 16 rows: workers, and units small enough for 32 bits over `tiles` tiles of at most `tokens` tokens.
 void plan_rows(Geometry* g, long long tiles, long long tokens) {
   g->workers = std::max(1, kWorkers / g->Hkv);
+  if (tiles * (tokens / kGrain) <= kFewUnits * g->workers) g->workers = std::max(1, g->workers / 2);
   g->grain = kGrain;
   while (tiles * (tokens / g->grain + 1 + kTileCost) >= (1ll << 30) - g->workers) g->grain *= 2;
   g->slots = tokens > g->grain ? 2 * g->workers : 0;  // else no border lies inside a tile
@@ -184,8 +189,7 @@ extern "C" {
 size_t pqc_paged_counter_bytes(const pqc_paged_config* cfg) {
   Geometry g;
   if (make_geometry(cfg, 1, &g) != PQC_OK) return 0;
-  plan_rows(&g, 1, 1);
-  return (size_t)g.workers * g.Hkv * sizeof(unsigned);
+  return (size_t)std::max(1, kWorkers / g.Hkv) * g.Hkv * sizeof(unsigned);  // of as many workers as any call has
 }
 
 size_t pqc_paged_workspace_bytes(const pqc_paged_config* cfg, int32_t n, int32_t n_idx) {

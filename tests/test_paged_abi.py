@@ -106,6 +106,16 @@ def test_workspace_grows_with_neither_tokens_nor_pages(lib):
     assert lib.pqc_paged_workspace_bytes(C.byref(config()), 2, 100) == 0
 
 
+def test_counters_are_enough_for_calls_of_any_size(lib):
+    # one word per border between workers and head; the most workers that any call has: 512 over all heads, one per head at least
+    for heads, words in ((1, 512), (2, 512), (3, 510), (8, 512), (96, 480), (600, 600)):
+        for most in (1, 16, 4096):
+            c = config(n_q_heads=heads, n_kv_heads=heads, max_pages=most)
+            assert lib.pqc_paged_counter_bytes(C.byref(c)) == 4 * words, (heads, most)
+    assert lib.pqc_paged_counter_bytes(C.byref(config(head_dim=80, rot_dims=64))) == 0
+    assert attn(lib, config(), pages(counters=P + 2)) == -1
+
+
 def test_the_binding_says_what_is_wrong():
     k = torch.zeros((4, 2, 16, 64), dtype=torch.bfloat16)
     cache = paged.PagedCache(k, k.clone(), None, None, n_q_heads=4)
