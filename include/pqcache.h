@@ -429,7 +429,8 @@ typedef struct pqc_paged_cache { /* device pointers, 16-byte aligned (page_table
  *                          (may be NULL; for pqc_pq_build, pqc_pq_encode_token): io_dtype,
  *                          not overlapping the inputs
  * A token goes to place lengths[b] - (tokens of b) + i of its sequence; places outside
- * [0, max_pages * page_tokens) are not stored.  The pages written to must be of one sequence each.
+ * [0, max_pages * page_tokens) are not stored.  A page written to must be named once
+ * in the table.
  * PQC_FP8: the scale of a (page, head), of keys and of values apart, is the smallest power of two
  * with which all its values are within the type's 448.  If a page's scale has to grow for new
  * tokens, its older codes are encoded anew, which a power of two leaves exact down to the
@@ -454,7 +455,8 @@ size_t pqc_paged_counter_bytes(const pqc_paged_config* cfg);
 
 /* Softmax attention of every query head over all cached tokens of its sequence up to the
  * query's own place (causal): query token i of the m of sequence b sees the tokens
- * t <= lengths[b] - m + i.  A query that sees none gives zeros.
+ * t <= lengths[b] - m + i.  A query that sees none gives zeros.  Sequences with one query token
+ * and sequences with many are quicker in calls of their own.
  *   q    [n][Hq][D] io_dtype     out  [n][Hq][D] out_dtype
  *   workspace  256-byte aligned, pqc_paged_workspace_bytes(cfg, n, 0); contents need not be
  *              kept, calls that share it must be ordered on one stream

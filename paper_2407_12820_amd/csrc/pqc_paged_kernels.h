@@ -770,6 +770,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(Geometry g, Cache c, 
         // barrier in front of the count, and what is read behind the count is read from there.
         const int w1 = (now.t.at + kTileCost) / share + 1;  // the first border inside the tile
         const int parts = (now.t.at + now.t.units - 1) / share - w1 + 2;
+        if (w1 >= g.workers) return;  // (offsets that do not ascend)
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
         if (threadIdx.x == 0) {

@@ -61,8 +61,13 @@ def rotation_table(n_positions: int, rot_dims: int, base: float = 10000.0, devic
 # quickest of torch's accessors, and what is wrong is worked out by _need and _rows only if something is.
 class PagedCache:
     """Pages [n_pages][Hkv][page_tokens][D] of keys and of values, float8_e4m3fn with scales [n_pages][Hkv] f32, or bfloat16
-    (scales None).  Like a decode context it is not thread-safe.  `dtype`: "f32" or "bf16", of q, k and v; `out_dtype`: of the attention output; `rotation`: the table of
-    rotation_table() or one laid out like it, None for no rotation."""
+    (scales None).  `dtype`: "f32" or "bf16", of q, k and v; `out_dtype`: of the attention output; `rotation`: the table of
+    rotation_table() or one laid out like it, None for no rotation.  Like a decode context it is not thread-safe.
+
+    Calls run on the current stream, or on `stream`, to which their allocations then belong too.  They may be recorded into
+    graphs; make one ordinary attention call before, so that the counters that save a launch exist."""
+
+    RECORDED = 32  # calls recorded into graphs that get counters of their own
 
     def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, k_scale: Optional[torch.Tensor], v_scale: Optional[torch.Tensor], *,
                  n_q_heads: int, dtype: str = "bf16", out_dtype: str = "f32", softmax_scale: float = 0.0,
@@ -95,7 +100,7 @@ class PagedCache:
         self._dev = k_pages.get_device()
         self._sizes = {}  # workspace bytes by (batch, listed tokens)
         # counters (pqc_paged_counter_bytes): one block per stream, and one of its own for each recorded call, so that neither two
-        # streams nor two graphs share any; without a block a call takes two launches
+        # streams nor two graphs share any; a call recorded before the first ordinary one, or beyond RECORDED, does without
         self._counters, self._spare, self._recorded = {}, [], []
 
     @classmethod
@@ -150,11 +155,11 @@ class PagedCache:
             self._need(t, dtype, (n, heads, self.dim), what)
         return t.data_ptr()
 
-    def _call(self, what: str, fn, stream, args) -> None:
-        """fn(*args, stream) with the cache's device current."""
+    def _call(self, what: str, fn, args) -> None:
+        """fn(*args, current stream) with the cache's device current."""
         if self._dev < 0:
             raise ValueError(f"{what} runs on a GPU, the pages are on {self.device}")
-        st = torch._C._cuda_getCurrentRawStream(self._dev) if stream is None else stream.cuda_stream
+        st = torch._C._cuda_getCurrentRawStream(self._dev)
         if torch._C._cuda_getDevice() == self._dev:
             rc = fn(*args, st)
         else:
@@ -163,39 +168,36 @@ class PagedCache:
         if rc != 0:
             raise PQCacheError(rc, what)
 
-    def _workspace(self, batch: int, n_idx: int, stream):
+    def _workspace(self, batch: int, n_idx: int):
+        """Workspace of an attention call on the current stream, allocated on that stream; sets the call's counters."""
+        if self._dev >= 0:
+            if torch._C._cuda_getDevice() == self._dev:
+                self._count()
+            else:
+                with torch.cuda.device(self._dev):
+                    self._count()
         size = self._sizes.get((batch, n_idx))
         if size is None:
             if len(self._sizes) >= 256:
                 self._sizes.clear()
             size = self._sizes[batch, n_idx] = self.lib.pqc_paged_workspace_bytes(self._cfg, batch, n_idx)
         if not size:
-            return None, None
+            return None, None, 0
         ws = torch.empty(size, dtype=torch.uint8, device=self.device)
-        if stream is not None and self._dev >= 0:
-            ws.record_stream(stream)  # not given to another tensor before the call has run there
-        return ws, ws.data_ptr()
+        return ws, ws.data_ptr(), size
 
-    def _count_on(self, stream) -> None:
-        """Sets the counters of an attention call on `stream` (None: the current one)."""
-        if self._dev < 0:
-            return
-        if stream is not None and stream.cuda_stream != torch._C._cuda_getCurrentRawStream(self._dev):
-            with torch.cuda.stream(stream):
-                return self._count_on(None)
+    def _count(self) -> None:
         if torch._C._cuda_isCurrentStreamCapturing():
-            if self._spare:
-                self._recorded.append(self._spare.pop())
-                self.pages.counters = self._recorded[-1].data_ptr()
-            else:
-                self.pages.counters = None
+            block = self._spare.pop() if self._spare else None
+            self._recorded.append(block)
+            self.pages.counters = None if block is None else block.data_ptr()
             return
         st = torch._C._cuda_getCurrentRawStream(self._dev)
         block = self._counters.get(st)
         if block is None:
-            words = self.lib.pqc_paged_counter_bytes(self._cfg) // 4
             fill = not self._counters
-            blocks = torch.zeros((33 if fill else 1, max(words, 1)), dtype=torch.int32, device=self.device)
+            words = max(self.lib.pqc_paged_counter_bytes(self._cfg) // 4, 1)
+            blocks = torch.zeros((1 + self.RECORDED if fill else 1, words), dtype=torch.int32, device=self.device)
             block = self._counters[st] = blocks[0]
             if fill:
                 self._spare = list(blocks[1:])
@@ -206,6 +208,9 @@ class PagedCache:
                positions=None, q_out=None, k_out=None, stream=None):
         """New tokens k, v [n][Hkv][D] (rows of a projection allowed) join their sequences; `lengths` counts them already.
         With q [n][Hq][D] returns its rotated copy (q_out if given); k_out, if given, receives the rotated keys."""
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.append(k, v, page_table, lengths, new_offsets=new_offsets, q=q, positions=positions, q_out=q_out, k_out=k_out)
         n, heads = k.shape[0], self.heads
         off = self._place(page_table, lengths, new_offsets, n)
         k_stride, v_stride = self._rows(k, n, heads, "k"), self._rows(v, n, heads, "v")
@@ -221,12 +226,15 @@ class PagedCache:
         if positions is not None:
             pos = self._need(positions, torch.int32, (n,), "positions")
         if n:
-            self._call("pqc_paged_append", self.lib.pqc_paged_append, stream,
+            self._call("pqc_paged_append", self.lib.pqc_paged_append,
                        (self._cfg, self._pages, qp, q_stride, k.data_ptr(), k_stride, v.data_ptr(), v_stride, n, off, pos, self._rotation, qo, ko))
         return q_out
 
     def attn(self, q: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor, *, q_offsets=None, out=None, stream=None):
         """Attention of q [n][Hq][D] over all tokens of each sequence, causal; -> out [n][Hq][D]."""
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.attn(q, page_table, lengths, q_offsets=q_offsets, out=out)
         n = q.shape[0]
         off = self._place(page_table, lengths, q_offsets, n)
         qp = self._plain(q, self.io, n, self.q_heads, "q")
@@ -234,13 +242,15 @@ class PagedCache:
             out = torch.empty((n, self.q_heads, self.dim), dtype=self.out, device=self.device)
         op = self._plain(out, self.out, n, self.q_heads, "out")
         if n:
-            self._count_on(stream)
-            ws, wp = self._workspace(self.cfg.batch, 0, stream)
-            self._call("pqc_paged_attn", self.lib.pqc_paged_attn, stream, (self._cfg, self._pages, qp, n, off, op, wp, 0 if ws is None else ws.numel()))
+            ws, wp, size = self._workspace(self.cfg.batch, 0)
+            self._call("pqc_paged_attn", self.lib.pqc_paged_attn, (self._cfg, self._pages, qp, n, off, op, wp, size))
         return out
 
     def gather_attn(self, q: torch.Tensor, idx: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor, *, out=None, stream=None):
         """Attention of q [B][Hq][D] over the tokens idx [B][Hkv][n_idx] int32 of each sequence; -> out [B][Hq][D]."""
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.gather_attn(q, idx, page_table, lengths, out=out)
         b = q.shape[0]
         self._place(page_table, lengths, None, b)
         qp = self._plain(q, self.io, b, self.q_heads, "q")
@@ -250,8 +260,6 @@ class PagedCache:
         if out is None:
             out = torch.empty((b, self.q_heads, self.dim), dtype=self.out, device=self.device)
         op = self._plain(out, self.out, b, self.q_heads, "out")
-        self._count_on(stream)
-        ws, wp = self._workspace(b, n_idx, stream)
-        self._call("pqc_paged_gather_attn", self.lib.pqc_paged_gather_attn, stream,
-                   (self._cfg, self._pages, qp, idx.data_ptr(), n_idx, op, wp, 0 if ws is None else ws.numel()))
+        ws, wp, size = self._workspace(b, n_idx)
+        self._call("pqc_paged_gather_attn", self.lib.pqc_paged_gather_attn, (self._cfg, self._pages, qp, idx.data_ptr(), n_idx, op, wp, size))
         return out

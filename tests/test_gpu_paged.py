@@ -115,6 +115,14 @@ MANY = [  # lengths, queries, P, heads, G, D, cache, dtype, out
     ([3000, 10], [3, 10], 64, 1, 4, 128, "fp8", "bf16", "f32"),             # a few queries on a long cache: splits
     ([1500, 700], [300, 650], 64, 2, 4, 128, "fp8", "bf16", "bf16"),
     ([900], [900], 16, 1, 8, 128, "bf16", "bf16", "f32"),
+    # tiles of 128 rows: groups that do not divide them, more queries than tokens, rows that see nothing, one long sequence of splits
+    ([130, 77], [130, 70], 16, 2, 3, 64, "fp8", "bf16", "f32"),
+    ([300, 20, 64, 0], [200, 90, 64, 3], 32, 1, 7, 128, "fp8", "bf16", "bf16"),
+    ([129, 1, 257], [129, 1, 200], 256, 1, 5, 128, "bf16", "bf16", "f32"),
+    ([200, 65], [150, 65], 64, 1, 6, 64, "bf16", "bf16", "bf16"),
+    ([5000, 63], [40, 63], 64, 1, 4, 128, "fp8", "bf16", "f32"),
+    ([6000], [33], 16, 1, 1, 128, "fp8", "bf16", "bf16"),
+    ([40], [40], 128, 1, 13, 64, "fp8", "bf16", "f32"),
 ]
 
 
@@ -138,7 +146,7 @@ def test_attention_of_several_tokens(paged, lengths, queries, P, heads, G, D, ca
     assert bool((res[off[-1]:] == 7.0).all()), "rows behind the last sequence"
 
 
-@pytest.mark.parametrize("several", [False, True])
+@pytest.mark.parametrize("several", [0, 3, 40])  # query tokens of each sequence (0: one, without offsets)
 def test_pages_that_are_not_there_and_lengths_out_of_range(paged, several):
     # entries outside the pool name no page: their tokens are left out; lengths are taken into the table's room
     gen = torch.Generator().manual_seed(5)
@@ -148,8 +156,8 @@ def test_pages_that_are_not_there_and_lengths_out_of_range(paged, several):
     table[2, :], table[3, 0] = -7, -2 ** 31
     told = torch.tensor([300, 200, 500, 2 ** 31 - 1], dtype=torch.int32)  # the last: all of its row, whose rear entries are -1
     told_cut = torch.tensor([300, 200, 500, table.shape[1] * 64])
-    n = 4 if not several else 12
-    off = torch.tensor([0, 3, 6, 9, 12], dtype=torch.int32) if several else None
+    n = 4 * several if several else 4
+    off = several * torch.arange(5, dtype=torch.int32) if several else None
     q = torch.randn((n, 8, 128), generator=gen).to(torch.bfloat16)
     # (the fourth sequence ends inside its third page; what lies behind would be read if its length were believed)
     for name in (0, 1):
@@ -435,7 +443,7 @@ def test_parts_folded_by_the_last_workgroup_or_by_a_kernel(paged, lengths, P, he
     torch.cuda.synchronize()
     blocks = list(c._counters.values())
     assert len(blocks) == 1 and not bool(blocks[0].any())
-    c._count_on = lambda stream: setattr(c.pages, "counters", None)
+    c._count = lambda: setattr(c.pages, "counters", None)
     own = [c.attn(dq, dt, lens) for _ in range(3)] + [c.gather_attn(dq, di, dt, lens) for _ in range(3)]
     torch.cuda.synchronize()
     few = [b for b in range(B) if lengths[b] < 5000][:3] + [0]
