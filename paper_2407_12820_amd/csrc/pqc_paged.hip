@@ -59,15 +59,18 @@ int make_geometry(const pqc_paged_config* c, long long n, Geometry* g) {
   g->out_bf16 = c->out_dtype == PQC_BF16;
   const float scale = c->softmax_scale > 0.0f ? c->softmax_scale : 1.0f / std::sqrt((float)c->head_dim);
   g->scale_log2e = scale * 1.4426950408889634f;
-  g->per_head = g->items = g->slots = g->workers = g->grain = 0;
+  g->per_head = g->least = g->items = g->slots = g->workers = g->grain = 0;
   return PQC_OK;
 }
 
 // What takes a call: a tile per query token, tiles of 16 rows, or (many queries per sequence) of 128 rows.
+// Tiles of 128 rows from 64 rows per sequence on (8 heads of 4 query heads; us with tiles of 16 and of 128: one sequence of 17482 tokens, 32
+// rows 33.1, 38.3, 64 40.1, 38.5, 96 49.8, 40.1, 256 85.6, 45.5; sixteen of 4096, 32 rows 48.7, 49.3, 64 70.7, 53.9).  Their splits are of
+// 512 tokens at least, since each leaves up to 64 KB of partial results (512 queries on themselves: splits of 256 26.8, of 512 19.0).
 enum class Tiles { kOne, kRows, kBlock };
 Tiles tiles_for(const pqc_paged_config* c, const Geometry& g, const int* offsets) {
   if (!offsets) return Tiles::kOne;
-  return c->io_dtype == PQC_BF16 && (long long)g.n_q * g.G >= 32ll * g.B ? Tiles::kBlock : Tiles::kRows;
+  return (long long)g.n_q * g.G >= 64ll * g.B ? Tiles::kBlock : Tiles::kRows;
 }
 // The kernel of 16 rows: workers, and units small enough for 32 bits over `tiles` tiles of at most `tokens` tokens.
 void plan_rows(Geometry* g, long long tiles, long long tokens) {
@@ -85,6 +88,7 @@ void plan_attn(Geometry* g, Tiles form) {
     return;
   }
   g->per_head = std::max(1, (kBlockItems + g->Hkv - 1) / g->Hkv);
+  g->least = 512;
   g->items = (int)tiles + g->per_head;
   g->slots = 2 * g->per_head;
 }
@@ -141,38 +145,45 @@ void launch_rows(const AttnCall& a) {
     hipLaunchKernelGGL((attn_fold_kernel<C, D>), dim3((unsigned)g.workers - 1, g.Hkv, g.R * g.G), dim3(256), 0, a.st, g, a.c.lengths,
                        a.offsets,                       LISTED ? a.n_idx : -1, a.partials, a.out);
 }
-template <class C, int D>
+template <typename T, class C, int D>
 void launch_block(const AttnCall& a) {
   const Geometry& g = a.g;
   const dim3 grid((unsigned)(g.items * g.Hkv));
   if (g.out_bf16)
-    hipLaunchKernelGGL((attn_block_kernel<C, D, 1>), grid, dim3(256), 0, a.st, g, a.c, static_cast<const bf16_t*>(a.q), a.offsets, a.out, a.partials);
+    hipLaunchKernelGGL((attn_block_kernel<T, C, D, 1>), grid, dim3(256), 0, a.st, g, a.c, static_cast<const T*>(a.q), a.offsets, a.out, a.partials);
   else
-    hipLaunchKernelGGL((attn_block_kernel<C, D, 3>), grid, dim3(256), 0, a.st, g, a.c, static_cast<const bf16_t*>(a.q), a.offsets, a.out, a.partials);
-  if ((g.max_pages << g.shift) > kGrain)
-    hipLaunchKernelGGL((attn_block_fold_kernel<D>), dim3((unsigned)std::min(g.per_head, g.items - g.per_head), g.Hkv, 4), dim3(256), 0, a.st, g,
-                       a.c.lengths, a.offsets, a.partials, a.out);
+    hipLaunchKernelGGL((attn_block_kernel<T, C, D, 3>), grid, dim3(256), 0, a.st, g, a.c, static_cast<const T*>(a.q), a.offsets, a.out, a.partials);
+  if ((g.max_pages << g.shift) <= g.least) return;  // no tile has several splits
+  // tiles of several splits have two items at least; few tiles are folded by many workgroups each
+  const int tiles = std::min(g.per_head, g.items - g.per_head), by = tiles * g.Hkv <= 128 ? 16 : 4;
+  hipLaunchKernelGGL((attn_block_fold_kernel<D>), dim3((unsigned)tiles, g.Hkv, by), dim3(256), 0, a.st, g, a.c.lengths, a.offsets, a.partials, a.out);
+}
+// f(a query's type, a codec), by the configuration's types
+template <class F>
+void by_types(const pqc_paged_config* cfg, F f) {
+  const bool f32 = cfg->io_dtype == PQC_F32, fp8 = cfg->cache_dtype == PQC_FP8;
+  if (f32 && fp8) f(float{}, Fp8{});
+  else if (f32) f(float{}, Bf16{});
+  else if (fp8) f(bf16_t{}, Fp8{});
+  else f(bf16_t{}, Bf16{});
 }
 int launch_blocks(const pqc_paged_config* cfg, const AttnCall& a) {
-  if (cfg->cache_dtype == PQC_FP8)
-    cfg->head_dim == 128 ? launch_block<Fp8, 128>(a) : launch_block<Fp8, 64>(a);
-  else
-    cfg->head_dim == 128 ? launch_block<Bf16, 128>(a) : launch_block<Bf16, 64>(a);
+  by_types(cfg, [&](auto t, auto c) {
+    if (cfg->head_dim == 128)
+      launch_block<decltype(t), decltype(c), 128>(a);
+    else
+      launch_block<decltype(t), decltype(c), 64>(a);
+  });
   return launched();
 }
 template <bool LISTED>
 int launch_attn(const pqc_paged_config* cfg, const AttnCall& a) {
-  auto by_dim = [&](auto t, auto c) {
+  by_types(cfg, [&](auto t, auto c) {
     if (cfg->head_dim == 128)
       launch_rows<decltype(t), decltype(c), 128, LISTED>(a);
     else
       launch_rows<decltype(t), decltype(c), 64, LISTED>(a);
-  };
-  const bool f32 = cfg->io_dtype == PQC_F32, fp8 = cfg->cache_dtype == PQC_FP8;
-  if (f32 && fp8) by_dim(float{}, Fp8{});
-  else if (f32) by_dim(float{}, Bf16{});
-  else if (fp8) by_dim(bf16_t{}, Fp8{});
-  else by_dim(bf16_t{}, Bf16{});
+  });
   return launched();
 }
 

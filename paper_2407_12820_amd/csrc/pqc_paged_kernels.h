@@ -28,7 +28,7 @@ struct Geometry {
   int n_pages, max_pages;
   int n_q;                // query (or new) tokens of all sequences
   int R;                  // query tokens per tile
-  int per_head;           // items per head that the split length aims at
+  int per_head, least;    // items per head that the split length aims at, and the shortest split
   int items, slots;       // bounds of the numbers of items and of partial results per head
   int workers, grain;     // kernel of 16 rows: workgroups per head, tokens of a unit of their work
   bool out_bf16;
@@ -80,7 +80,7 @@ __device__ __forceinline__ int split_tokens(const Geometry& g, const int* length
   }
   // a little more than the quotient, so that rounding keeps the number of items within its bound
   const float tokens = ceilf(wave_sum(work) * 1.001f / (float)(g.per_head * kGrain));
-  return max(1, (int)fminf(tokens, 1e7f)) * kGrain;
+  return max(g.least, max(1, (int)fminf(tokens, 1e7f)) * kGrain);
 }
 // The j-th item, or the j-th tile of more than one split (whole_tiles); b < 0: there are fewer.
 __device__ __forceinline__ Item find_item(const Geometry& g, const int* lengths, const int* offsets, int j, bool whole_tiles) {
@@ -934,7 +934,7 @@ __global__ __launch_bounds__(256) void attn_block_fold_kernel(Geometry g, const 
     if (qr >= it.s.nq) return;
     float m = kNegBig, l = 0.0f;
     f32x4_t o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
+#pragma unroll 8
     for (int i = 0; i < it.n_split; ++i) {
       const float* p = base + i * stride;
       const float2 ml = *reinterpret_cast<const float2*>(p + rows * D + 2 * r);
@@ -961,8 +961,9 @@ __global__ __launch_bounds__(256) void attn_block_fold_kernel(Geometry g, const 
 // unit (one alone takes 1.4 times as long).  Prompts of 8192 tokens, 32 query heads, 8 KV heads: 590 us, 930 TFLOP/s; round after
 // round without the overlap 634; operands read one instruction ahead instead of four 604.  64 rows per wave, which would halve the
 // reads of LDS, need more registers than the vector ALU reaches and spend the gain on copies.
-template <class C, int D, int TERMS>
-__global__ __launch_bounds__(256, 2) void attn_block_kernel(Geometry g, Cache c, const bf16_t* __restrict__ q, const int* __restrict__ offsets,
+template <typename T, class C, int D, int TERMS>
+__global__ __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) void attn_block_kernel(Geometry g, Cache c, const T* __restrict__ q,
+                                                                                            const int* __restrict__ offsets,
                                                             void* __restrict__ out, float* __restrict__ partials) {
   __shared__ __align__(16) unsigned char lds_k[2][kBlockTokens * D * 2], lds_v[2][kBlockTokens * D * 2];
   __shared__ unsigned present[2];  // a byte per 16 tokens of keys: their page is there
@@ -980,14 +981,33 @@ __global__ __launch_bounds__(256, 2) void attn_block_kernel(Geometry g, Cache c,
   const int row0 = 32 * wave, row1 = min(row0 + 31, g.R * g.G - 1);
   const int least = row0 < g.R * g.G ? hidden + it.tile * g.R + row0 / g.G + 1 : 0;
   const int wave_most = row0 < g.R * g.G ? min(most, hidden + it.tile * g.R + row1 / g.G + 1) : 0;
-  bf16x8_t qf[D / 16];
+  constexpr int kQ = sizeof(T) == 4 ? 3 : 1;  // bf16 terms of a query's value
+  bf16x8_t qf[kQ][D / 16];
   {
-    const bf16_t* row = q + ((size_t)(it.s.first + qi) * g.Hq + (size_t)h * g.G + r % g.G) * D + 8 * half;
+    const T* row = q + ((size_t)(it.s.first + qi) * g.Hq + (size_t)h * g.G + r % g.G) * D + 8 * half;
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) {
-      u32x4_t x = {0u, 0u, 0u, 0u};
-      if (row_ok) x = *reinterpret_cast<const u32x4_t*>(row + 16 * i);
-      __builtin_memcpy(&qf[i], &x, 16);
+      if constexpr (kQ == 1) {
+        u32x4_t x = {0u, 0u, 0u, 0u};
+        if (row_ok) x = *reinterpret_cast<const u32x4_t*>(row + 16 * i);
+        __builtin_memcpy(&qf[0][i], &x, 16);
+      } else {
+        f32x4_t x[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+        if (row_ok) {
+          x[0] = *reinterpret_cast<const f32x4_t*>(row + 16 * i);
+          x[1] = *reinterpret_cast<const f32x4_t*>(row + 16 * i + 4);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          float y = x[e >> 2][e & 3];
+#pragma unroll
+          for (int t = 0; t < kQ; ++t) {
+            const __bf16 b = (__bf16)y;
+            qf[t][i][e] = b;
+            y -= (float)b;
+          }
+        }
+      }
     }
   }
   f32x16_t o[D / 32];
@@ -1044,16 +1064,18 @@ __global__ __launch_bounds__(256, 2) void attn_block_kernel(Geometry g, Cache c,
 #pragma unroll
       for (int e = 0; e < D / 16; ++e)
 #pragma unroll
-        for (int b = 0; b < 2; ++b) s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[2 * e + b], qf[e], s[b], 0, 0, 0);
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int t = 0; t < kQ; ++t) s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[2 * e + b], qf[t][e], s[b], 0, 0, 0);
       // operands are read kAhead instructions ahead
 #pragma unroll
       for (int e = 0; e < kAhead; ++e) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
 #pragma unroll
       for (int e = 0; e < 2 * (D / 16) - kAhead; ++e) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, kQ, 0);
         __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
       }
-      __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, kQ * kAhead, 0);
     };
     auto mask = [&](int i) {
       const int t = t0 + i * kBlockTokens;
@@ -1208,7 +1230,7 @@ __global__ __launch_bounds__(256, 2) void attn_block_kernel(Geometry g, Cache c,
   }
   const u32x2_t both = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
   l = __uint_as_float(both[0]) + __uint_as_float(both[1]);
-  if (r >= g.R * g.G) return;
+  if (!row_ok) return;
   if (it.slot >= 0) {
     const int rows = g.R * g.G;
     float* po = partials + ((size_t)(it.slot + it.split) * g.Hkv + h) * partial_floats(rows, D);
@@ -1222,7 +1244,6 @@ __global__ __launch_bounds__(256, 2) void attn_block_kernel(Geometry g, Cache c,
     }
     return;
   }
-  if (!row_ok) return;
   const float inv = l > 0.0f ? 1.0f / l : 0.0f;
   const size_t at = ((size_t)(it.s.first + qi) * g.Hq + (size_t)h * g.G + r % g.G) * D + 4 * half;
 #pragma unroll

@@ -123,6 +123,8 @@ MANY = [  # lengths, queries, P, heads, G, D, cache, dtype, out
     ([5000, 63], [40, 63], 64, 1, 4, 128, "fp8", "bf16", "f32"),
     ([6000], [33], 16, 1, 1, 128, "fp8", "bf16", "bf16"),
     ([40], [40], 128, 1, 13, 64, "fp8", "bf16", "f32"),
+    ([300, 140, 9], [300, 33, 20], 64, 1, 4, 128, "fp8", "f32", "f32"),
+    ([170, 2500], [170, 31], 128, 2, 3, 128, "bf16", "f32", "bf16"),
 ]
 
 
