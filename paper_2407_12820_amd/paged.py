@@ -1,8 +1,11 @@
 """Paged key/value cache: ctypes marshalling over the pqc_paged_* calls of include/pqcache.h.
 
 A `PagedCache` is a view of a pool of pages that the caller owns: which sequences lie in it, and where, comes with every
-call as a page table and lengths, so that one object serves a batch that changes from step to step.  Workspaces are
-allocated per call from torch's caching allocator, hence two streams, or two captured graphs, share none.
+call as a page table and lengths, so that one object serves a batch that changes from step to step.
+
+Scratch memory of the attention calls: one workspace and one block of counters per stream, which all caches share, since
+what runs on a stream runs in order.  A call that is recorded into a graph has a workspace out of the graph's own memory and
+counters that no other call gets, so that two graphs share none.
 """
 from __future__ import annotations
 
@@ -50,6 +53,40 @@ def _load():
     return _lib
 
 
+class _Scratch:
+    """Of one stream."""
+
+    def __init__(self, device, words: int):
+        self.counters = torch.zeros(words, dtype=torch.int32, device=device)
+        self.counters_ptr = self.counters.data_ptr()
+        self.workspace, self.ptr, self.size = None, 0, 0
+
+    def grow(self, size: int) -> None:
+        self.workspace = torch.empty(size, dtype=torch.uint8, device=self.counters.device)
+        self.ptr, self.size = self.workspace.data_ptr(), size
+
+
+class _Device:
+    """Scratch memory of a GPU: by raw stream, and counters for recorded calls."""
+
+    RECORDED = 64  # recorded calls that get counters of their own; later ones take a launch more
+    WORDS = 512    # counters that a call of up to 512 KV heads needs
+
+    def __init__(self):
+        self.streams, self.spare, self.recorded = {}, [], []
+
+    def stream(self, raw: int, device) -> _Scratch:
+        found = self.streams.get(raw)
+        if found is None:
+            if not self.streams:
+                self.spare = list(torch.zeros((self.RECORDED, self.WORDS), dtype=torch.int32, device=device))
+            found = self.streams[raw] = _Scratch(device, self.WORDS)
+        return found
+
+
+_devices = {}
+
+
 def rotation_table(n_positions: int, rot_dims: int, base: float = 10000.0, device="cuda:0") -> torch.Tensor:
     """[n_positions][rot_dims] f32: cosines, then sines, of position * base^(-2j / rot_dims); angles in double precision."""
     j = torch.arange(0, rot_dims, 2, device=device, dtype=torch.float64)
@@ -66,8 +103,6 @@ class PagedCache:
 
     Calls run on the current stream, or on `stream`, to which their allocations then belong too.  They may be recorded into
     graphs; make one ordinary attention call before, so that the counters that save a launch exist."""
-
-    RECORDED = 32  # calls recorded into graphs that get counters of their own
 
     def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, k_scale: Optional[torch.Tensor], v_scale: Optional[torch.Tensor], *,
                  n_q_heads: int, dtype: str = "bf16", out_dtype: str = "f32", softmax_scale: float = 0.0,
@@ -98,10 +133,10 @@ class PagedCache:
                            v_scale.data_ptr() if fp8 else None, None, None, None)
         self._cfg, self._pages = C.byref(self.cfg), C.byref(self.pages)
         self._dev = k_pages.get_device()
+        self._scratch = _devices.setdefault(self._dev, _Device())
+        self._counted = 0 < self.lib.pqc_paged_counter_bytes(self._cfg) <= 4 * _Device.WORDS
         self._sizes = {}  # workspace bytes by (batch, listed tokens)
-        # counters (pqc_paged_counter_bytes): one block per stream, and one of its own for each recorded call, so that neither two
-        # streams nor two graphs share any; a call recorded before the first ordinary one, or beyond RECORDED, does without
-        self._counters, self._spare, self._recorded = {}, [], []
+        self._set = (1, 1, None, None, None)  # batch, max_pages, page table, lengths and counters as they are in the structures
 
     @classmethod
     def empty(cls, n_pages: int, n_q_heads: int, n_kv_heads: int, head_dim: int = 128, page_tokens: int = 64, cache_dtype: str = "fp8",
@@ -140,9 +175,15 @@ class PagedCache:
             self._need(lengths, torch.int32, (b,), "lengths")
         if page_table.dtype is not torch.int32 or not page_table.is_contiguous() or page_table.get_device() != self._dev:
             self._need(page_table, torch.int32, shape, "page_table")
-        cfg, pages = self.cfg, self.pages
-        cfg.batch, cfg.max_pages = b, most
-        pages.page_table, pages.lengths = page_table.data_ptr(), lengths.data_ptr()
+        was_b, was_most, was_table, was_lengths, counters = self._set
+        table, lens = page_table.data_ptr(), lengths.data_ptr()
+        if b != was_b or most != was_most:
+            self.cfg.batch, self.cfg.max_pages = b, most
+        if table != was_table:
+            self.pages.page_table = table
+        if lens != was_lengths:
+            self.pages.lengths = lens
+        self._set = b, most, table, lens, counters
         if offsets is not None:
             return self._need(offsets, torch.int32, (b + 1,), "offsets")
         if n != b:
@@ -155,53 +196,40 @@ class PagedCache:
             self._need(t, dtype, (n, heads, self.dim), what)
         return t.data_ptr()
 
-    def _call(self, what: str, fn, args) -> None:
-        """fn(*args, current stream) with the cache's device current."""
-        if self._dev < 0:
+    def _attend(self, what: str, fn, batch: int, n_idx: int, args) -> None:
+        """fn(*args, workspace, bytes, stream) on the current stream of the cache's device."""
+        dev = self._dev
+        if dev < 0:
             raise ValueError(f"{what} runs on a GPU, the pages are on {self.device}")
-        st = torch._C._cuda_getCurrentRawStream(self._dev)
-        if torch._C._cuda_getDevice() == self._dev:
-            rc = fn(*args, st)
-        else:
-            with torch.cuda.device(self._dev):
-                rc = fn(*args, st)
-        if rc != 0:
-            raise PQCacheError(rc, what)
-
-    def _workspace(self, batch: int, n_idx: int):
-        """Workspace of an attention call on the current stream, allocated on that stream; sets the call's counters."""
-        if self._dev >= 0:
-            if torch._C._cuda_getDevice() == self._dev:
-                self._count()
-            else:
-                with torch.cuda.device(self._dev):
-                    self._count()
-        size = self._sizes.get((batch, n_idx))
-        if size is None:
+        if torch._C._cuda_getDevice() != dev:
+            with torch.cuda.device(dev):
+                return self._attend(what, fn, batch, n_idx, args)
+        need = self._sizes.get((batch, n_idx))
+        if need is None:
             if len(self._sizes) >= 256:
                 self._sizes.clear()
-            size = self._sizes[batch, n_idx] = self.lib.pqc_paged_workspace_bytes(self._cfg, batch, n_idx)
-        if not size:
-            return None, None, 0
-        ws = torch.empty(size, dtype=torch.uint8, device=self.device)
-        return ws, ws.data_ptr(), size
-
-    def _count(self) -> None:
+            need = self._sizes[batch, n_idx] = self.lib.pqc_paged_workspace_bytes(self._cfg, batch, n_idx)
+        raw = torch._C._cuda_getCurrentRawStream(dev)
         if torch._C._cuda_isCurrentStreamCapturing():
-            block = self._spare.pop() if self._spare else None
-            self._recorded.append(block)
-            self.pages.counters = None if block is None else block.data_ptr()
-            return
-        st = torch._C._cuda_getCurrentRawStream(self._dev)
-        block = self._counters.get(st)
-        if block is None:
-            fill = not self._counters
-            words = max(self.lib.pqc_paged_counter_bytes(self._cfg) // 4, 1)
-            blocks = torch.zeros((1 + self.RECORDED if fill else 1, words), dtype=torch.int32, device=self.device)
-            block = self._counters[st] = blocks[0]
-            if fill:
-                self._spare = list(blocks[1:])
-        self.pages.counters = block.data_ptr()
+            own = self._scratch.spare.pop() if self._scratch.spare and self._counted else None
+            self._scratch.recorded.append(own)  # the graph's for good
+            counters = None if own is None else own.data_ptr()
+            workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
+            at, size = workspace.data_ptr(), need
+        else:
+            scratch = self._scratch.streams.get(raw)
+            if scratch is None:
+                scratch = self._scratch.stream(raw, self.device)
+            if scratch.size < need:
+                scratch.grow(need)
+            counters = scratch.counters_ptr if self._counted else None
+            at, size = scratch.ptr, scratch.size
+        if counters != self._set[4]:
+            self.pages.counters = counters
+            self._set = (*self._set[:4], counters)
+        rc = fn(*args, at, size, raw)
+        if rc != 0:
+            raise PQCacheError(rc, what)
 
     # -- entry points (same names as the C ABI)
     def append(self, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor, *, new_offsets=None, q=None,
@@ -226,8 +254,15 @@ class PagedCache:
         if positions is not None:
             pos = self._need(positions, torch.int32, (n,), "positions")
         if n:
-            self._call("pqc_paged_append", self.lib.pqc_paged_append,
-                       (self._cfg, self._pages, qp, q_stride, k.data_ptr(), k_stride, v.data_ptr(), v_stride, n, off, pos, self._rotation, qo, ko))
+            if self._dev < 0:
+                raise ValueError(f"pqc_paged_append runs on a GPU, the pages are on {self.device}")
+            if torch._C._cuda_getDevice() != self._dev:
+                with torch.cuda.device(self._dev):
+                    return self.append(k, v, page_table, lengths, new_offsets=new_offsets, q=q, positions=positions, q_out=q_out, k_out=k_out)
+            rc = self.lib.pqc_paged_append(self._cfg, self._pages, qp, q_stride, k.data_ptr(), k_stride, v.data_ptr(), v_stride, n, off, pos,
+                                           self._rotation, qo, ko, torch._C._cuda_getCurrentRawStream(self._dev))
+            if rc != 0:
+                raise PQCacheError(rc, "pqc_paged_append")
         return q_out
 
     def attn(self, q: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor, *, q_offsets=None, out=None, stream=None):
@@ -242,8 +277,7 @@ class PagedCache:
             out = torch.empty((n, self.q_heads, self.dim), dtype=self.out, device=self.device)
         op = self._plain(out, self.out, n, self.q_heads, "out")
         if n:
-            ws, wp, size = self._workspace(self.cfg.batch, 0)
-            self._call("pqc_paged_attn", self.lib.pqc_paged_attn, (self._cfg, self._pages, qp, n, off, op, wp, size))
+            self._attend("pqc_paged_attn", self.lib.pqc_paged_attn, lengths.shape[0], 0, (self._cfg, self._pages, qp, n, off, op))
         return out
 
     def gather_attn(self, q: torch.Tensor, idx: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor, *, out=None, stream=None):
@@ -260,6 +294,5 @@ class PagedCache:
         if out is None:
             out = torch.empty((b, self.q_heads, self.dim), dtype=self.out, device=self.device)
         op = self._plain(out, self.out, b, self.q_heads, "out")
-        ws, wp, size = self._workspace(b, n_idx)
-        self._call("pqc_paged_gather_attn", self.lib.pqc_paged_gather_attn, (self._cfg, self._pages, qp, idx.data_ptr(), n_idx, op, wp, size))
+        self._attend("pqc_paged_gather_attn", self.lib.pqc_paged_gather_attn, b, n_idx, (self._cfg, self._pages, qp, idx.data_ptr(), n_idx, op))
         return out
