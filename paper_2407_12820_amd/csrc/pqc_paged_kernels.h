@@ -958,7 +958,7 @@ __global__ __launch_bounds__(256) void attn_block_fold_kernel(Geometry g, const 
 // The vector ALU has about as much to do as the matrix cores (64 tokens, one wave: 32 exponentials and some 200 other instructions,
 // 1000 to 1300 cycles, against 32 matrix instructions of 32), so the two run side by side within a wave: the weights of a round's tokens
 // are computed while the values of the round before are multiplied, keys being a round ahead of values.  Two workgroups share a compute
-// unit (one alone takes 1.4 times as long).  Prompts of 8192 tokens, 32 query heads, 8 KV heads: 590 us, 930 TFLOP/s; round after
+// unit (one alone takes 1.4 times as long).  Prompts of 8192 tokens, 32 query heads, 8 KV heads: 581 us, 945 TFLOP/s; round after
 // round without the overlap 634; operands read one instruction ahead instead of four 604.  64 rows per wave, which would halve the
 // reads of LDS, need more registers than the vector ALU reaches and spend the gain on copies.
 template <typename T, class C, int D, int TERMS>
