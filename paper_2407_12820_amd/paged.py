@@ -135,7 +135,7 @@ class PagedCache:
         self._dev = k_pages.get_device()
         self._scratch = _devices.setdefault(self._dev, _Device())
         self._counted = 0 < self.lib.pqc_paged_counter_bytes(self._cfg) <= 4 * _Device.WORDS
-        self._sizes = {}  # workspace bytes by (batch, listed tokens)
+        self._sizes = {}  # workspace bytes by (query tokens, listed tokens, batch, max_pages)
         self._set = (1, 1, None, None, None)  # batch, max_pages, page table, lengths and counters as they are in the structures
 
     @classmethod
@@ -196,19 +196,20 @@ class PagedCache:
             self._need(t, dtype, (n, heads, self.dim), what)
         return t.data_ptr()
 
-    def _attend(self, what: str, fn, batch: int, n_idx: int, args) -> None:
+    def _attend(self, what: str, fn, n: int, n_idx: int, args) -> None:
         """fn(*args, workspace, bytes, stream) on the current stream of the cache's device."""
         dev = self._dev
         if dev < 0:
             raise ValueError(f"{what} runs on a GPU, the pages are on {self.device}")
         if torch._C._cuda_getDevice() != dev:
             with torch.cuda.device(dev):
-                return self._attend(what, fn, batch, n_idx, args)
-        need = self._sizes.get((batch, n_idx))
+                return self._attend(what, fn, n, n_idx, args)
+        sizes = (n, n_idx, *self._set[:2])
+        need = self._sizes.get(sizes)
         if need is None:
             if len(self._sizes) >= 256:
                 self._sizes.clear()
-            need = self._sizes[batch, n_idx] = self.lib.pqc_paged_workspace_bytes(self._cfg, batch, n_idx)
+            need = self._sizes[sizes] = self.lib.pqc_paged_workspace_bytes(self._cfg, n, n_idx)
         raw = torch._C._cuda_getCurrentRawStream(dev)
         if torch._C._cuda_isCurrentStreamCapturing():
             own = self._scratch.spare.pop() if self._scratch.spare and self._counted else None
@@ -277,7 +278,7 @@ class PagedCache:
             out = torch.empty((n, self.q_heads, self.dim), dtype=self.out, device=self.device)
         op = self._plain(out, self.out, n, self.q_heads, "out")
         if n:
-            self._attend("pqc_paged_attn", self.lib.pqc_paged_attn, lengths.shape[0], 0, (self._cfg, self._pages, qp, n, off, op))
+            self._attend("pqc_paged_attn", self.lib.pqc_paged_attn, n, 0, (self._cfg, self._pages, qp, n, off, op))
         return out
 
     def gather_attn(self, q: torch.Tensor, idx: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor, *, out=None, stream=None):

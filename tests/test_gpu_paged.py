@@ -542,3 +542,17 @@ def test_random_shapes(paged):
         got = c.attn(dev(q), dev(table), dev(torch.tensor(lengths, dtype=torch.int32)), q_offsets=dev(off))
         torch.cuda.synchronize()
         close(got, *ref.attention(q, pages, table, torch.tensor(lengths), off, D ** -0.5, out), f"case {i}")
+
+
+def test_a_refused_call_leaves_later_ones_alone(paged):
+    # a table wider than 2^24 tokens is refused on the host; the next call of the same batch has its workspace all the same
+    c, _, table = make(paged, torch.Generator().manual_seed(3), [300], 16, 2, 4, 64, "fp8", "bf16", "f32")
+    q, lens = torch.randn((1, 8, 64), device=DEV).to(torch.bfloat16), torch.tensor([300], dtype=torch.int32, device=DEV)
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    c._scratch.streams.pop(stream.cuda_stream, None)
+    with pytest.raises(paged.PQCacheError):
+        c.attn(q, torch.full((1, (1 << 20) + 1), -1, dtype=torch.int32, device=DEV), lens, stream=stream)
+    got = c.attn(q, dev(table), lens, stream=stream)
+    torch.cuda.synchronize()
+    assert torch.equal(got, c.attn(q, dev(table), lens))
