@@ -10,6 +10,7 @@ counters that no other call gets, so that two graphs share none.
 from __future__ import annotations
 
 import ctypes as C
+import threading
 from typing import Optional
 
 import torch
@@ -85,6 +86,7 @@ class _Device:
 
 
 _devices = {}
+_lock = threading.Lock()  # from the choice of scratch memory to the launch: another thread may let it grow, which frees it
 
 
 def rotation_table(n_positions: int, rot_dims: int, base: float = 10000.0, device="cuda:0") -> torch.Tensor:
@@ -210,7 +212,11 @@ class PagedCache:
             if len(self._sizes) >= 256:
                 self._sizes.clear()
             need = self._sizes[sizes] = self.lib.pqc_paged_workspace_bytes(self._cfg, n, n_idx)
-        raw = torch._C._cuda_getCurrentRawStream(dev)
+        with _lock:
+            self._launch(what, fn, need, args)
+
+    def _launch(self, what: str, fn, need: int, args) -> None:
+        raw = torch._C._cuda_getCurrentRawStream(self._dev)
         if torch._C._cuda_isCurrentStreamCapturing():
             own = self._scratch.spare.pop() if self._scratch.spare and self._counted else None
             self._scratch.recorded.append(own)  # the graph's for good

@@ -556,3 +556,35 @@ def test_a_refused_call_leaves_later_ones_alone(paged):
     got = c.attn(q, dev(table), lens, stream=stream)
     torch.cuda.synchronize()
     assert torch.equal(got, c.attn(q, dev(table), lens))
+
+
+def test_threads_on_one_stream_keep_their_scratch_until_the_launch(paged):
+    import threading
+
+    c, _, table = make(paged, torch.Generator().manual_seed(4), [300], 16, 2, 4, 64, "fp8", "bf16", "f32")
+    d, _, _ = make(paged, torch.Generator().manual_seed(4), [300], 16, 2, 4, 64, "fp8", "bf16", "f32")
+    q, lens = torch.zeros((1, 8, 64), dtype=torch.bfloat16, device=DEV), torch.tensor([300], dtype=torch.int32, device=DEV)
+    dt, stream = dev(table), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    c._scratch.streams.pop(stream.cuda_stream, None)
+    kept, failed = [], []
+
+    def other():
+        try:
+            d.attn(q, dt, lens, stream=stream)  # needs more than the call below
+        except Exception as e:
+            failed.append(e)
+
+    def launch(at, size, raw):  # in place of a launch: nothing runs
+        thread.start()
+        thread.join(0.5)
+        kept.append(c._scratch.streams[raw].ptr == at)
+        return 0
+
+    thread = threading.Thread(target=other)
+    with torch.cuda.stream(stream):
+        c._place(dt, lens, None, 1)
+        c._attend("a call", launch, 1, 300, ())
+    thread.join()
+    torch.cuda.synchronize()
+    assert kept == [True] and not failed
