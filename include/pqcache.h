@@ -457,7 +457,7 @@ size_t pqc_paged_counter_bytes(const pqc_paged_config* cfg);
  * query's own place (causal): query token i of the m of sequence b sees the tokens
  * t <= lengths[b] - m + i.  A query that sees none gives zeros.  Sequences with one query token
  * and sequences with many are quicker in calls of their own.
- *   q    [n][Hq][D] io_dtype     out  [n][Hq][D] out_dtype
+ *   q    [n][Hq][D] io_dtype     out  [n][Hq][D] out_dtype, not overlapping the inputs
  *   workspace  256-byte aligned, pqc_paged_workspace_bytes(cfg, n, 0); contents need not be
  *              kept, calls that share it must be ordered on one stream
  * Sums, maxima and softmax weights are fp32; for a bf16 output the weights of calls with offsets may

@@ -192,6 +192,10 @@ class PagedCache:
             raise ValueError(f"{n} tokens for {b} sequences: give the offsets")
         return None
 
+    def _own(self, stream) -> None:
+        if stream.device != self.device:
+            raise ValueError(f"the stream is of {stream.device}, the pages are on {self.device}")
+
     def _plain(self, t: torch.Tensor, dtype, n: int, heads: int, what: str) -> int:
         """Address of a contiguous [n][heads][D]."""
         if t.dtype is not dtype or t.shape != (n, heads, self.dim) or not t.is_contiguous() or t.get_device() != self._dev:
@@ -244,6 +248,7 @@ class PagedCache:
         """New tokens k, v [n][Hkv][D] (rows of a projection allowed) join their sequences; `lengths` counts them already.
         With q [n][Hq][D] returns its rotated copy (q_out if given); k_out, if given, receives the rotated keys."""
         if stream is not None:
+            self._own(stream)
             with torch.cuda.stream(stream):
                 return self.append(k, v, page_table, lengths, new_offsets=new_offsets, q=q, positions=positions, q_out=q_out, k_out=k_out)
         n, heads = k.shape[0], self.heads
@@ -275,6 +280,7 @@ class PagedCache:
     def attn(self, q: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor, *, q_offsets=None, out=None, stream=None):
         """Attention of q [n][Hq][D] over all tokens of each sequence, causal; -> out [n][Hq][D]."""
         if stream is not None:
+            self._own(stream)
             with torch.cuda.stream(stream):
                 return self.attn(q, page_table, lengths, q_offsets=q_offsets, out=out)
         n = q.shape[0]
@@ -283,6 +289,8 @@ class PagedCache:
         if out is None:
             out = torch.empty((n, self.q_heads, self.dim), dtype=self.out, device=self.device)
         op = self._plain(out, self.out, n, self.q_heads, "out")
+        if op == qp and n:
+            raise ValueError("out must not overlap q")
         if n:
             self._attend("pqc_paged_attn", self.lib.pqc_paged_attn, n, 0, (self._cfg, self._pages, qp, n, off, op))
         return out
@@ -290,6 +298,7 @@ class PagedCache:
     def gather_attn(self, q: torch.Tensor, idx: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor, *, out=None, stream=None):
         """Attention of q [B][Hq][D] over the tokens idx [B][Hkv][n_idx] int32 of each sequence; -> out [B][Hq][D]."""
         if stream is not None:
+            self._own(stream)
             with torch.cuda.stream(stream):
                 return self.gather_attn(q, idx, page_table, lengths, out=out)
         b = q.shape[0]
@@ -301,5 +310,7 @@ class PagedCache:
         if out is None:
             out = torch.empty((b, self.q_heads, self.dim), dtype=self.out, device=self.device)
         op = self._plain(out, self.out, b, self.q_heads, "out")
+        if op == qp and b:
+            raise ValueError("out must not overlap q")
         self._attend("pqc_paged_gather_attn", self.lib.pqc_paged_gather_attn, b, n_idx, (self._cfg, self._pages, qp, idx.data_ptr(), n_idx, op))
         return out

@@ -153,3 +153,21 @@ def test_rotation_table():
     angle = 999.0 * 500000.0 ** (-2.0 * 5 / 64)
     assert abs(float(t[999, 5]) - torch.tensor(angle, dtype=torch.float64).cos().item()) < 1e-7
     assert abs(float(t[999, 32 + 5]) - torch.tensor(angle, dtype=torch.float64).sin().item()) < 1e-7
+
+
+def test_streams_of_other_devices_and_outputs_over_inputs_are_refused():
+    from types import SimpleNamespace
+
+    k = torch.zeros((4, 2, 16, 64), dtype=torch.bfloat16)
+    cache = paged.PagedCache(k, k.clone(), None, None, n_q_heads=4, out_dtype="bf16")
+    table, lengths = torch.zeros((2, 2), dtype=torch.int32), torch.ones(2, dtype=torch.int32)
+    x, q, idx = (torch.zeros((2, h, 64), dtype=torch.bfloat16) for h in (2, 4, 2))
+    idx = idx[:, :, :5].int().contiguous()
+    far = SimpleNamespace(device=torch.device("cuda", 1))
+    for call in (lambda: cache.append(x, x, table, lengths, stream=far), lambda: cache.attn(q, table, lengths, stream=far),
+                 lambda: cache.gather_attn(q, idx, table, lengths, stream=far)):
+        with pytest.raises(ValueError, match="stream"):
+            call()
+    for call in (lambda: cache.attn(q, table, lengths, out=q), lambda: cache.gather_attn(q, idx, table, lengths, out=q)):
+        with pytest.raises(ValueError, match="overlap"):
+            call()
