@@ -385,7 +385,8 @@ int pqc_block_cache_update(const pqc_config* cfg, int32_t block_tokens, int32_t 
  * token per sequence (n == B).
  * Supported: head_dim 64 or 128; up to 16 query heads per KV head, any number; page_tokens
  * 16, 32, 64, 128 or 256; cache_dtype PQC_BF16 or PQC_FP8; max_pages * page_tokens <= 2^24;
- * n_pages * Hkv * page_tokens < 2^31; B, Hkv <= 65535; n * Hq < 2^31. */
+ * n_pages * Hkv * page_tokens < 2^31; B, Hkv <= 65535; n * Hq < 2^31,
+ * and calls that fit a launch of 2^24 workgroups (else PQC_EUNSUPPORTED). */
 typedef struct pqc_paged_config {
   int32_t batch;         /* B                                                        */
   int32_t n_q_heads;     /* Hq                                                       */

@@ -13,6 +13,9 @@ using namespace pqc::paged;
 
 bool aligned(const void* p, unsigned n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
+// A launch takes fewer than 2^32 work items, workgroups have 256.
+constexpr long long kMaxGroups = 1ll << 24;
+
 // Workgroups of the kernel of 16 rows over all heads: two per compute unit.  One per compute unit leaves its start and its tiles' ends
 // uncovered (48 ragged sequences, 8 heads of 8 query heads, 280 MB: 80.5 us, two 70.4, three 79.9; a single sequence of 131072 tokens 64.9, 59.0,
 // 66.9).  kRowsLds, beyond the kernel's own arrays, keeps a third off a compute unit: with room for three the 512 are spread unevenly (8
@@ -224,7 +227,7 @@ int pqc_paged_attn(const pqc_paged_config* cfg, const pqc_paged_cache* cache, co
   const size_t need = attn_bytes(cfg, g);
   const Tiles form = tiles_for(cfg, g, offsets);
   plan_attn(&g, form);
-  if ((long long)g.items * g.Hkv >= (1ll << 31)) return PQC_EUNSUPPORTED;
+  if ((long long)g.items * g.Hkv >= kMaxGroups) return PQC_EUNSUPPORTED;
   if (!workspace || !aligned(workspace, 256) || workspace_bytes < need) return PQC_EWORKSPACE;
   if (n == 0) return PQC_OK;
   const Cache c = device_cache(cache);
@@ -278,7 +281,7 @@ int pqc_paged_append(const pqc_paged_config* cfg, const pqc_paged_cache* cache, 
   a.q_tokens = n >= 1024 ? 2 : 1;
   // a sequence of m tokens touches at most 1 + (m + P - 2) / P pages, and no more than m
   const long long pages = offsets ? std::min<long long>(n, (long long)n / g.P + 2ll * g.B) : n;
-  if (pages * 2 * g.Hkv + n >= (1ll << 31)) return PQC_EUNSUPPORTED;
+  if (pages * 2 * g.Hkv + (q ? (n + a.q_tokens - 1) / a.q_tokens : 0) >= kMaxGroups) return PQC_EUNSUPPORTED;
   a.kv_items = (int)pages;
   const Cache c = device_cache(cache);
   hipStream_t st = static_cast<hipStream_t>(stream);

@@ -171,3 +171,11 @@ def test_streams_of_other_devices_and_outputs_over_inputs_are_refused():
     for call in (lambda: cache.attn(q, table, lengths, out=q), lambda: cache.gather_attn(q, idx, table, lengths, out=q)):
         with pytest.raises(ValueError, match="overlap"):
             call()
+
+
+def test_calls_that_no_launch_takes_are_refused(lib):
+    # 2^32 work items: 2^25 tokens are 8.4 million workgroups for keys and values and 16.8 million for queries
+    assert append(lib, config(), pages(), n=1 << 25, offsets=P) == -2
+    # tiles of 128 rows of 65535 sequences, 300 heads
+    c = config(batch=65535, n_q_heads=300, n_kv_heads=300)
+    assert attn(lib, c, pages(), n=64 * 65535, offsets=P) == -2
