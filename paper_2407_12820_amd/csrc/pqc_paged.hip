@@ -16,6 +16,12 @@ bool aligned(const void* p, unsigned n) { return (reinterpret_cast<uintptr_t>(p)
 // A launch takes fewer than 2^32 work items, workgroups have 256.
 constexpr long long kMaxGroups = 1ll << 24;
 
+// Pages of a call from which append lays eight pages' workgroups of one head side by side.  Workgroups go to the eight dies in turn, so that the
+// heads of a page then share a die's L2 and its rotation angles, which else every die reads by itself (eight heads, 32768 tokens: 554 MB read, 436
+// so, 419 needed).  us without and with it, 32 query heads, 8 KV heads, pages of 64: 4096 tokens (64 pages) 19.9, 19.1, 8192 42.9, 40.0, 32768 161.3,
+// 152.4; pages of 256 187.0, 159.9; 2 KV heads 74.7, 73.7.  Fewer pages would be rounded up to workgroups without work.
+constexpr int kTogether = 64;
+
 // Workgroups of the kernel of 16 rows over all heads: two per compute unit.  One per compute unit leaves its start and its tiles' ends
 // uncovered (48 ragged sequences, 8 heads of 8 query heads, 280 MB: 80.5 us, two 70.4, three 79.9; a single sequence of 131072 tokens 64.9, 59.0,
 // 66.9).  kRowsLds, beyond the kernel's own arrays, keeps a third off a compute unit: with room for three the 512 are spread unevenly (8
@@ -277,10 +283,12 @@ int pqc_paged_append(const pqc_paged_config* cfg, const pqc_paged_cache* cache, 
   a.pairs = cfg->rot_style == PQC_ROT_PAIRS;
   a.q_out = q_out; a.k_out = k_out;
   // Query tokens per workgroup: two share a workgroup's heads as soon as there are several workgroups per compute unit (32768 tokens, 32 query
-  // heads, 8 KV heads: one 175 us, two 161, four 162, eight 168, 32 197; 4096 tokens 20.3, 19.9, 20.3, 21.6).
+  // heads, 8 KV heads: one 175 us, two 161, four 162, eight 168, 32 197; 4096 tokens 20.3, 19.9, 20.3, 21.6; before pages were put together).
   a.q_tokens = n >= 1024 ? 2 : 1;
   // a sequence of m tokens touches at most 1 + (m + P - 2) / P pages, and no more than m
-  const long long pages = offsets ? std::min<long long>(n, (long long)n / g.P + 2ll * g.B) : n;
+  long long pages = offsets ? std::min<long long>(n, (long long)n / g.P + 2ll * g.B) : n;
+  a.together = pages >= kTogether ? 8 : 1;
+  pages = (pages + a.together - 1) / a.together * a.together;
   if (pages * 2 * g.Hkv + (q ? (n + a.q_tokens - 1) / a.q_tokens : 0) >= kMaxGroups) return PQC_EUNSUPPORTED;
   a.kv_items = (int)pages;
   const Cache c = device_cache(cache);

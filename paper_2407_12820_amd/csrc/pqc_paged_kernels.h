@@ -1268,6 +1268,7 @@ struct AppendArgs {
   bool pairs;                 // (2j, 2j + 1) are rotated together, else (j, j + rot / 2)
   void *q_out, *k_out;        // [T][heads][D]
   int kv_items;               // bound of the number of (sequence, page) pairs
+  int together;          // pages of which the workgroups of one head lie side by side; divides kv_items
   int q_tokens;               // query tokens per workgroup
 };
 
@@ -1427,7 +1428,8 @@ __global__ __launch_bounds__(256) void append_kernel(Geometry g, Cache c, Append
     append_queries<T, D>(g, c, a, offsets, (int)blockIdx.x - kv_groups);
     return;
   }
-  const int j = blockIdx.x / (2 * g.Hkv), which = blockIdx.x - j * 2 * g.Hkv;
+  const int chunk = blockIdx.x / (2 * g.Hkv * a.together), in_chunk = blockIdx.x - chunk * 2 * g.Hkv * a.together;
+  const int which = in_chunk / a.together, j = chunk * a.together + in_chunk % a.together;
   const bool is_key = which < g.Hkv;
   const int h = is_key ? which : which - g.Hkv;
   // the j-th touched page
