@@ -461,8 +461,8 @@ size_t pqc_paged_counter_bytes(const pqc_paged_config* cfg);
  *   q    [n][Hq][D] io_dtype     out  [n][Hq][D] out_dtype, not overlapping the inputs
  *   workspace  256-byte aligned, pqc_paged_workspace_bytes(cfg, n, 0); contents need not be
  *              kept, calls that share it must be ordered on one stream
- * Sums, maxima and softmax weights are fp32; for a bf16 output the weights of calls with offsets may
- * enter the product with the values rounded to bf16. */
+ * Sums, maxima and softmax weights are fp32; weights enter the product with the values whole, or, for
+ * a bf16 output of calls with offsets, to within 2^-17. */
 int pqc_paged_attn(const pqc_paged_config* cfg, const pqc_paged_cache* cache, const void* q, int32_t n,
                    const int32_t* offsets, void* out, void* workspace, size_t workspace_bytes, void* stream);
 

@@ -159,7 +159,7 @@ void launch_block(const AttnCall& a) {
   const Geometry& g = a.g;
   const dim3 grid((unsigned)(g.items * g.Hkv));
   if (g.out_bf16)
-    hipLaunchKernelGGL((attn_block_kernel<T, C, D, 1>), grid, dim3(256), 0, a.st, g, a.c, static_cast<const T*>(a.q), a.offsets, a.out, a.partials);
+    hipLaunchKernelGGL((attn_block_kernel<T, C, D, 2>), grid, dim3(256), 0, a.st, g, a.c, static_cast<const T*>(a.q), a.offsets, a.out, a.partials);
   else
     hipLaunchKernelGGL((attn_block_kernel<T, C, D, 3>), grid, dim3(256), 0, a.st, g, a.c, static_cast<const T*>(a.q), a.offsets, a.out, a.partials);
   if ((g.max_pages << g.shift) <= g.least) return;  // no tile has several splits

@@ -342,7 +342,7 @@ struct State {
 // One step: logits of 32 tokens, one rescaling if a maximum grew, weights, values.  `see(tile, i)` says whether the lane's query
 // sees its i-th token of the tile, `live(tile, i)` whether any query of the tile does (else its value row may hold anything, NaN
 // among it, and is taken as zero); both only matter if `masked` (wave-uniform).  The weights enter as three bf16 terms,
-// whose sum is the fp32 weight: two leave out up to 2^-18 of it, which was the largest error of all over a few tokens (1.1e-6 of
+// whose sum is the fp32 weight: two leave out up to 2^-17 of it, which was the largest error of all over a few tokens (1.1e-6 of
 // the result against 1e-7), and the third is free where the bytes of the rows are what the step waits for.
 constexpr int kTerms = 3;
 // `next_k` and `next_v` request the rows of the wave's next step as soon as this step's are no longer needed.
@@ -953,14 +953,16 @@ __global__ __launch_bounds__(256) void attn_block_fold_kernel(Geometry g, const 
   }
 }
 
-// TERMS: bf16 terms of a weight: one where the output is bf16 (2^-9 of a weight, no more than the output's own rounding), three
-// for an fp32 output.
-// The vector ALU has about as much to do as the matrix cores (64 tokens, one wave: 32 exponentials and some 200 other instructions,
-// 1000 to 1300 cycles, against 32 matrix instructions of 32), so the two run side by side within a wave: the weights of a round's tokens
+// TERMS: bf16 terms of a weight: three, which is all of it, for an fp32 output, two for a bf16 output (2^-17 of a weight, of the output's own
+// rounding a 512th).  One, 2^-8, moves a bf16 output by as much again as its rounding does: prompts of 8192 tokens 2.1e-3 off 64 bits,
+// with two 1.63e-3, which is the rounding alone, for 1.3 times the time.
+// The vector ALU has about as much to do as the matrix cores (64 tokens, one wave: 32 exponentials and some 300 other instructions
+// against 48 matrix instructions of 32 cycles), so the two run side by side within a wave: the weights of a round's tokens
 // are computed while the values of the round before are multiplied, keys being a round ahead of values.  Two workgroups share a compute
-// unit (one alone takes 1.4 times as long).  Prompts of 8192 tokens, 32 query heads, 8 KV heads: 581 us, 945 TFLOP/s; round after
-// round without the overlap 634; operands read one instruction ahead instead of four 604.  64 rows per wave, which would halve the
-// reads of LDS, need more registers than the vector ALU reaches and spend the gain on copies.
+// unit (one alone takes 1.4 times as long).  Prompts of 8192 tokens, 32 query heads, 8 KV heads: 757 us, 726 TFLOP/s, for an fp32
+// output 931.  (Measured with one term, 581 us: round after round without the overlap 634; operands read one instruction ahead instead of
+// four 604.)  Splitting weights into terms as they are computed instead of in front of their product: 766.  64 rows per wave, which
+// would halve the reads of LDS, need more registers than the vector ALU reaches and spend the gain on copies.
 template <typename T, class C, int D, int TERMS>
 __global__ __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) void attn_block_kernel(Geometry g, Cache c, const T* __restrict__ q,
                                                                                             const int* __restrict__ offsets,
@@ -1044,7 +1046,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) void attn_
     };
     constexpr int kAhead = 4;
     f32x16_t s[2];
-    unsigned w[TERMS == 1 ? 16 : 32];  // weights of a round: pairs of bf16, or fp32 until they are multiplied
+    float w[32];  // weights of a round, fp32 until they are multiplied
     // Where the lane reads its operands; the chunk of an instruction is an exclusive or with its number (worked out anew in each
     // round: sixteen addresses kept in registers leave too few for operands read ahead).
     unsigned k_at = col * (D * 2) + ((half ^ (col & 7)) << 4), v_at = col * 128 + ((half ^ ((col ^ (col >> 2)) & 7)) << 4);
@@ -1120,39 +1122,23 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) void attn_
     };
     auto weigh = [&](int b, int k) {  // 16 tokens
 #pragma unroll
-      for (int e = 8 * k; e < 8 * k + 8; e += 2) {
-        const float p0 = __builtin_amdgcn_exp2f(s[b][e]), p1 = __builtin_amdgcn_exp2f(s[b][e + 1]);
-        if constexpr (TERMS == 1) {
-          const unsigned u = w[8 * b + e / 2] = pack_bf16(p0, p1);
-          bf16x2_t p, one = {(__bf16)1.0f, (__bf16)1.0f};
-          __builtin_memcpy(&p, &u, 4);
-          l = __builtin_amdgcn_fdot2_f32_bf16(p, one, l, false);  // the sum of the weights as they are multiplied
-        } else {
-          l += p0 + p1;
-          w[16 * b + e] = __float_as_uint(p0);
-          w[16 * b + e + 1] = __float_as_uint(p1);
-        }
-      }
+      for (int e = 8 * k; e < 8 * k + 8; ++e) l += w[16 * b + e] = __builtin_amdgcn_exp2f(s[b][e]);
     };
     auto multiply = [&](int i, int b, int k) {
       bf16x8_t p[TERMS];
-      if constexpr (TERMS == 1) {
-        __builtin_memcpy(&p[0], &w[8 * b + 4 * k], 16);
-      } else {
-        u32x4_t x[TERMS];
+      u32x4_t x[TERMS];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float p0 = __uint_as_float(w[16 * b + 8 * k + 2 * e]), p1 = __uint_as_float(w[16 * b + 8 * k + 2 * e + 1]);
+      for (int e = 0; e < 4; ++e) {
+        float p0 = w[16 * b + 8 * k + 2 * e], p1 = w[16 * b + 8 * k + 2 * e + 1];
 #pragma unroll
-          for (int y = 0; y < TERMS; ++y) {
-            x[y][e] = pack_bf16(p0, p1);
-            p0 -= __uint_as_float(x[y][e] << 16);
-            p1 -= __uint_as_float(x[y][e] & 0xffff0000u);
-          }
+        for (int y = 0; y < TERMS; ++y) {
+          x[y][e] = pack_bf16(p0, p1);
+          p0 -= __uint_as_float(x[y][e] << 16);
+          p1 -= __uint_as_float(x[y][e] & 0xffff0000u);
         }
-#pragma unroll
-        for (int y = 0; y < TERMS; ++y) __builtin_memcpy(&p[y], &x[y], 16);
       }
+#pragma unroll
+      for (int y = 0; y < TERMS; ++y) __builtin_memcpy(&p[y], &x[y], 16);
 #pragma unroll
       for (int n = 0; n < D / 32; ++n) {
         bf16x8_t v;
