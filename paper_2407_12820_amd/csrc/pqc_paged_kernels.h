@@ -438,6 +438,10 @@ __device__ __forceinline__ void store_out(const Geometry& g, void* out, size_t a
     static_cast<float*>(out)[at] = x;
 }
 
+// Of a row's softmax weights.  0 for a row that saw nothing; a sum that is not a number stays one (a NaN in the query or in a key that it sees,
+// a logit of +inf), whichever kernel comes to it.
+__device__ __forceinline__ float reciprocal_sum(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
+
 // A barrier for LDS alone: loads from memory stay in flight across it.
 __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
@@ -517,7 +521,7 @@ __device__ __forceinline__ void fold_parts(const Geometry& g, const Seq& s, int 
     }
     if (side == 0 && live) {
       const size_t a = ((size_t)(s.first + qr) * g.Hq + (size_t)h * g.G + r % g.G) * D + 4 * at;
-      o *= l > 0.0f ? 1.0f / l : 0.0f;
+      o *= reciprocal_sum(l);
       if (g.out_bf16)
         *reinterpret_cast<u32x2_t*>(static_cast<bf16_t*>(out) + a) = u32x2_t{pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};
       else
@@ -762,7 +766,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(Geometry g, Cache c, 
           }
         } else {
           const int qr = now.t.tile * g.R + r / g.G;
-          if (qr < now.t.s.nq) store_out(g, out, ((size_t)(now.t.s.first + qr) * g.Hq + (size_t)h * g.G + r % g.G) * D + d, sum > 0.0f ? o / sum : 0.0f);
+          if (qr < now.t.s.nq) store_out(g, out, ((size_t)(now.t.s.first + qr) * g.Hq + (size_t)h * g.G + r % g.G) * D + d, sum == 0.0f ? 0.0f : o / sum);  // as reciprocal_sum
         }
       }
       if (!whole && c.counters) {
@@ -945,7 +949,7 @@ __global__ __launch_bounds__(256) void attn_block_fold_kernel(Geometry g, const 
       o = o * corr + f * x;
     }
     const size_t a = ((size_t)(it.s.first + qr) * g.Hq + (size_t)h * g.G + r % g.G) * D + 4 * at;
-    o *= l > 0.0f ? 1.0f / l : 0.0f;
+    o *= reciprocal_sum(l);
     if (g.out_bf16)
       *reinterpret_cast<u32x2_t*>(static_cast<bf16_t*>(out) + a) = u32x2_t{pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};
     else
@@ -1230,7 +1234,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) void attn_
     }
     return;
   }
-  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+  const float inv = reciprocal_sum(l);
   const size_t at = ((size_t)(it.s.first + qi) * g.Hq + (size_t)h * g.G + r % g.G) * D + 4 * half;
 #pragma unroll
   for (int n = 0; n < D / 32; ++n)

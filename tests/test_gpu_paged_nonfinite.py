@@ -1,0 +1,134 @@
+"""GPU tests of NaN and infinities around the paged cache: they reach the results they belong to, and no others."""
+import pytest
+import torch
+
+import paged_reference as ref
+from test_gpu_paged import DEV, IO, close, dev, make, paged, place  # noqa: F401  (paged: fixture)
+
+pytestmark = pytest.mark.gpu
+
+# ------------------------------------------------------------------ attention
+SHAPES = {  # lengths, query tokens per sequence (0: one, without offsets), listed tokens, heads, G: which way a tile goes
+    "one, whole": ([50, 90], 0, 0, 2, 4),
+    "one, folded": ([2048, 700], 0, 0, 8, 4),
+    "one, folded by a kernel": ([20011, 700], 0, 0, 1, 4),
+    "listed, whole": ([300, 90], 0, 60, 2, 4),
+    "listed, folded": ([2500, 1800], 0, 1700, 8, 4),
+    "rows, whole": ([100, 60], 6, 0, 2, 4),
+    "rows, folded": ([6000, 3000], 6, 0, 2, 4),
+    "block, whole": ([300, 150], 70, 0, 2, 4),
+    "block, split": ([5000, 700], 50, 0, 1, 4),
+}
+
+
+class Call:
+    """One call of a shape on finite inputs, whose keys, values and queries a test then spoils."""
+
+    def __init__(self, paged, shape, cache, dtype="bf16", out="f32", seed=1):
+        self.lengths, self.several, count, self.heads, self.G = SHAPES[shape]
+        self.gen = torch.Generator().manual_seed(seed)
+        self.c, self.pages, self.table = make(paged, self.gen, self.lengths, 64, self.heads, self.G, 128, cache, dtype, out)
+        B = len(self.lengths)
+        self.offsets = self.several * torch.arange(B + 1, dtype=torch.int32) if self.several else None
+        self.m = self.several or 1
+        self.q = torch.randn((B * self.m, self.heads * self.G, 128), generator=self.gen).to(IO[dtype])
+        self.out = out
+        self.idx = None
+        if count:
+            self.idx = torch.full((B, self.heads, count), -1, dtype=torch.int32)
+            for b, t in enumerate(self.lengths):
+                self.idx[b, :, :min(t, count)] = torch.randperm(t, generator=self.gen)[:count].int()
+
+    def run(self):
+        lens = dev(torch.tensor(self.lengths, dtype=torch.int32))
+        if self.idx is not None:
+            return self.c.gather_attn(dev(self.q), dev(self.idx), dev(self.table), lens)
+        return self.c.attn(dev(self.q), dev(self.table), lens, q_offsets=dev(self.offsets))
+
+    def expected(self):
+        return ref.attention(self.q, self.pages, self.table, torch.tensor(self.lengths), self.offsets, 128 ** -0.5, self.out, listed=self.idx)
+
+    def spoil(self, name, b, token, h, dim=None, value=float("nan")):
+        """One value, or all, of a cached row on the device; what the reference reads stays finite."""
+        pool = self.c.k_pages if name == "k" else self.c.v_pages
+        page, slot = int(self.table[b, token // 64]), token % 64
+        row = pool[page, h, slot].float()
+        row[slice(None) if dim is None else dim] = value
+        pool[page, h, slot] = row.to(pool.dtype)
+
+    def seeing(self, b, token, h):
+        """Rows [n][Hq] of sequence b and KV head h that see the token."""
+        sees = torch.zeros(self.q.shape[:2], dtype=torch.bool)
+        for i in range(self.m):
+            if token <= self.lengths[b] - self.m + i:
+                sees[b * self.m + i, h * self.G:(h + 1) * self.G] = True
+        return sees
+
+
+def check(call, spoiled, what):
+    """Rows `spoiled` ([n][Hq], or with a last axis of dimensions) are NaN, the others as they were."""
+    want, tol = call.expected()
+    got = call.run()
+    torch.cuda.synchronize()
+    mask = (spoiled if spoiled.dim() == 3 else spoiled[..., None]).expand_as(want)
+    nan = torch.isnan(got.cpu())
+    assert bool(nan[mask].all()), f"{what}: {int((~nan[mask]).sum())} of {int(mask.sum())} values are not NaN"
+    close(got, want.masked_fill(mask, float("nan")), tol, what)
+
+
+@pytest.mark.parametrize("cache", ["fp8", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_a_query_that_is_not_a_number(paged, shape, cache):
+    call = Call(paged, shape, cache)
+    row = call.q.shape[0] - 1 if call.m == 1 else 2
+    print(f"[case] {shape} {cache}", flush=True)
+    spoiled = torch.zeros(call.q.shape[:2], dtype=torch.bool)
+    spoiled[row, 1] = True
+    want = call.expected()
+    call.expected = lambda: want
+    call.q[row, 1, 77] = float("nan")
+    check(call, spoiled, shape)
+
+
+@pytest.mark.parametrize("cache", ["fp8", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_a_key_that_is_not_a_number(paged, shape, cache):
+    call = Call(paged, shape, cache)
+    last = call.lengths[0] - 1
+    tokens = [int(call.idx[0, 1, 3])] if call.idx is not None else [last] if call.m == 1 else [last - 2]  # the last two or three queries see it
+    h = call.heads - 1
+    print(f"[case] {shape} {cache}", flush=True)
+    if call.idx is not None:
+        tokens = [int(call.idx[0, h, 3])]
+    call.spoil("k", 0, tokens[0], h, dim=5)
+    check(call, call.seeing(0, tokens[0], h), shape)
+    call.spoil("k", 0, 0 if call.idx is None else tokens[0], h, dim=9)  # and one that all of them see
+    check(call, call.seeing(0, 0, h), shape)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_an_infinite_logit(paged, shape, dtype):
+    # exp(inf - inf): the softmax of a row with a logit of +inf is not a number
+    call = Call(paged, shape, "bf16", dtype)
+    call.q[..., 5] = call.q[..., 5].abs() + 0.5
+    h, token = call.heads - 1, call.lengths[0] // 2
+    if call.idx is not None:
+        token = int(call.idx[0, h, 7])
+    print(f"[case] {shape} {dtype}", flush=True)
+    call.spoil("k", 0, token, h, dim=5, value=float("inf"))
+    check(call, call.seeing(0, token, h), shape)
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("cache", ["fp8", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_a_value_that_is_not_a_number(paged, shape, cache, out):
+    call = Call(paged, shape, cache, out=out)
+    h, token = call.heads - 1, 0
+    if call.idx is not None:
+        token = int(call.idx[0, h, 7])
+    print(f"[case] {shape} {cache} {out}", flush=True)
+    call.spoil("v", 0, token, h, dim=37)
+    spoiled = call.seeing(0, token, h)[..., None] & (torch.arange(128) == 37)
+    check(call, spoiled, shape)
