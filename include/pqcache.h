@@ -433,7 +433,8 @@ typedef struct pqc_paged_cache { /* device pointers, 16-byte aligned (page_table
  * [0, max_pages * page_tokens) are not stored.  A page written to must be named once
  * in the table.
  * PQC_FP8: the scale of a (page, head), of keys and of values apart, is the smallest power of two
- * with which all its values are within the type's 448.  If a page's scale has to grow for new
+ * (2^-100 at least) with which all its finite values are within the type's 448; a value that is
+ * infinite or not a number is stored as the type's NaN.  If a page's scale has to grow for new
  * tokens, its older codes are encoded anew, which a power of two leaves exact down to the
  * type's subnormals.  A page that receives its first token starts anew, whatever it held. */
 int pqc_paged_append(const pqc_paged_config* cfg, const pqc_paged_cache* cache, const void* q, int64_t q_stride,

@@ -1293,7 +1293,10 @@ __device__ __forceinline__ void store8(T* p, const float (&x)[8]) {
     __builtin_nontemporal_store(f32x4_t{x[4], x[5], x[6], x[7]}, reinterpret_cast<f32x4_t*>(p + 4));
   }
 }
-// Eight e4m3 codes of x * inv, |x * inv| <= 448 (nearest even).
+// What a scale is chosen by: an infinity would leave the other values of its page no codes but zero, so that it becomes the type's NaN like a
+// NaN itself, and the scale is that of the finite values.
+__device__ __forceinline__ float finite_size(float x) { return fabsf(x) < INFINITY ? fabsf(x) : 0.0f; }
+// Eight e4m3 codes of x * inv, |x * inv| <= 448 (nearest even), or NaN of what is not finite.
 __device__ __forceinline__ u32x2_t encode8(const float (&x)[8], float inv) {
   u32x2_t w;
 #pragma unroll
@@ -1485,7 +1488,7 @@ __global__ __launch_bounds__(256) void append_kernel(Geometry g, Cache c, Append
     float lo[kHeld][8], hi[kHeld][8], amax = 0.0f;
     auto largest = [&](const float (&x)[8], const float (&y)[8]) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fmaxf(fabsf(x[e]), fabsf(y[e])));
+      for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fmaxf(finite_size(x[e]), finite_size(y[e])));
     };
 #pragma unroll
     for (int e = 0; e < kHeld; ++e)

@@ -132,3 +132,61 @@ def test_a_value_that_is_not_a_number(paged, shape, cache, out):
     call.spoil("v", 0, token, h, dim=37)
     spoiled = call.seeing(0, token, h)[..., None] & (torch.arange(128) == 37)
     check(call, spoiled, shape)
+
+
+# ------------------------------------------------------------------ append
+def is_nan_code(pages):
+    return (pages.view(torch.uint8) & 0x7F) == 0x7F
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_an_infinity_leaves_the_other_tokens_of_its_page(paged, dtype, D):
+    """Scales are those of the finite values; what is not finite is a NaN of the type, in its own places alone."""
+    gen = torch.Generator().manual_seed(8)
+    P, heads, inf = 64, 2, float("inf")
+    c = paged.PagedCache.empty(2, heads, heads, D, P, dtype=dtype, device=DEV)
+    table = torch.tensor([[1]], dtype=torch.int32, device=DEV)
+    x = torch.randn((60, heads, D), generator=gen)
+    x[41] *= 8.0                                 # the scale grows in the same call as the infinities come
+    bad = torch.zeros_like(x, dtype=torch.bool)
+    for at, value in (((40, 0, 3), inf), ((41, 0, D - 1), -inf), ((41, 1, 17), inf), ((45, 1, 20), float("nan"))):
+        x[at], bad[at] = value, True
+    x[50, 0], bad[50, 0] = -inf, True            # a token without a finite value
+    x = x.to(IO[dtype])
+    done = 0
+    for n in (20, 20, 2, 1, 5, 1, 1, 1, 9):      # the page's first call, then ones on top of what it holds
+        part = dev(x[done:done + n].contiguous())
+        done += n
+        off = torch.tensor([0, n], dtype=torch.int32, device=DEV)
+        c.append(part, part, table, torch.tensor([done], dtype=torch.int32, device=DEV), new_offsets=off)
+    torch.cuda.synchronize()
+    finite = x[:done].double().masked_fill(bad[:done], 0.0)
+    for pool, scale in ((c.k_pages, c.k_scale), (c.v_pages, c.v_scale)):
+        got = ref.dequantised(pool.cpu(), scale.cpu())[1].transpose(0, 1)[:done]
+        assert torch.equal(is_nan_code(pool.cpu())[1].transpose(0, 1)[:done], bad[:done])
+        for h in range(heads):
+            s = ref.power_scale(float(finite[:, h].abs().max()))
+            assert float(scale[1, h]) == s
+            want = finite[:, h]
+            # as in a page that is filled token by token: half a step of e4m3, less than one step of the last subnormals
+            err = (got[:, h] - want).abs().masked_fill(bad[:done, h], 0.0)
+            assert bool((err <= 2.0 ** -4 * want.abs() + 2.0 ** -9 * s).all())
+
+
+def test_a_page_that_begins_with_an_infinity(paged):
+    gen = torch.Generator().manual_seed(9)
+    c = paged.PagedCache.empty(1, 1, 1, 64, 16, device=DEV)
+    c.k_scale.fill_(float("nan"))
+    x = torch.randn((2, 1, 64), generator=gen).to(torch.bfloat16)
+    first = torch.full((1, 1, 64), float("inf"), dtype=torch.bfloat16)
+    table, at = torch.zeros((1, 1), dtype=torch.int32, device=DEV), lambda n: torch.tensor([n], dtype=torch.int32, device=DEV)
+    c.append(dev(first), dev(first), table, at(1))
+    assert bool(is_nan_code(c.k_pages)[0, 0, 0].all()) and float(c.k_scale) == 2.0 ** -100
+    for i in range(2):
+        c.append(dev(x[i:i + 1]), dev(x[i:i + 1]), table, at(2 + i))
+    torch.cuda.synchronize()
+    s = ref.power_scale(float(x.double().abs().max()))
+    assert float(c.k_scale) == s and bool(is_nan_code(c.k_pages)[0, 0, 0].all())
+    got = ref.dequantised(c.k_pages.cpu(), c.k_scale.cpu())[0, 0, 1:3]
+    assert bool(((got - x[:, 0].double()).abs() <= 2.0 ** -4 * x[:, 0].double().abs() + 2.0 ** -9 * s).all())
