@@ -457,8 +457,9 @@ size_t pqc_paged_counter_bytes(const pqc_paged_config* cfg);
 
 /* Softmax attention of every query head over all cached tokens of its sequence up to the
  * query's own place (causal): query token i of the m of sequence b sees the tokens
- * t <= lengths[b] - m + i.  A query that sees none gives zeros.  Sequences with one query token
- * and sequences with many are quicker in calls of their own.
+ * t <= lengths[b] - m + i.  A query that sees none gives zeros; tokens that it does not see leave it
+ * alone, whatever they hold (NaN and infinities included).  Sequences with one query token and
+ * sequences with many are quicker in calls of their own.
  *   q    [n][Hq][D] io_dtype     out  [n][Hq][D] out_dtype, not overlapping the inputs
  *   workspace  256-byte aligned, pqc_paged_workspace_bytes(cfg, n, 0); contents need not be
  *              kept, calls that share it must be ordered on one stream

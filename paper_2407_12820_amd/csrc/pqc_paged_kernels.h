@@ -254,6 +254,13 @@ struct Fp8 {
   // dimensions 2j, 2j + 1 of the lane's chunk as a pair of bf16
   template <int N>
   __device__ static __forceinline__ unsigned pair(const unsigned (&v)[N], int j) { return two(v[j >> 1], (j & 1) != 0); }
+  // the bits of a word's values that are not finite
+  __device__ static __forceinline__ unsigned odd(unsigned w) {
+    const unsigned t = ~w & 0x7f7f7f7fu;  // zero where the value is
+    return ((~(t + 0x7f7f7f7fu) & 0x80808080u) >> 7) * 0xffu;
+  }
+  // value `dim` of a row if it is not finite, else zero
+  __device__ static __forceinline__ float odd_value(const unsigned char* row, int dim) { return (row[dim] & 0x7f) == 0x7f ? __builtin_nanf("") : 0.0f; }
 };
 struct Bf16 {
   static constexpr int kBytes = 2;
@@ -269,7 +276,17 @@ struct Bf16 {
   }
   template <int N>
   __device__ static __forceinline__ unsigned pair(const unsigned (&v)[N], int j) { return v[j]; }
+  __device__ static __forceinline__ unsigned odd(unsigned w) {
+    const unsigned t = ~w & 0x7f807f80u;
+    return ((~(t + 0x7fff7fffu) & 0x80008000u) >> 15) * 0xffffu;
+  }
+  __device__ static __forceinline__ float odd_value(const unsigned char* row, int dim) {
+    const unsigned x = reinterpret_cast<const uint16_t*>(row)[dim];
+    return (x & 0x7f80u) == 0x7f80u ? __uint_as_float(x << 16) : 0.0f;
+  }
 };
+// Tokens that some queries of a tile see and others do not have a weight of zero for the others, which an infinity or NaN among their values would
+// turn into NaN.  Such values are taken out of the product (`odd`) and added to the queries that see them by themselves (`odd_value`).
 
 template <class C, int D>
 struct Stage {
@@ -345,10 +362,11 @@ struct State {
 // whose sum is the fp32 weight: two leave out up to 2^-17 of it, which was the largest error of all over a few tokens (1.1e-6 of
 // the result against 1e-7), and the third is free where the bytes of the rows are what the step waits for.
 constexpr int kTerms = 3;
-// `next_k` and `next_v` request the rows of the wave's next step as soon as this step's are no longer needed.
-template <typename T, class C, int D, class SeeFn, class LiveFn, class KsFn, class VsFn, class NextK, class NextV>
-__device__ __forceinline__ void attend(Stage<C, D>& st, const Query<T, C, D>& q, State<D>& a, bool masked, SeeFn see, LiveFn live, KsFn ks, VsFn vs,
-                                       NextK next_k, NextV next_v) {
+// `next_k` and `next_v` request the rows of the wave's next step as soon as this step's are no longer needed.  `partly` (wave-uniform, and masked
+// then): some queries may not see what others see; `add_odd` adds the tokens' values that are not finite.
+template <typename T, class C, int D, class SeeFn, class LiveFn, class KsFn, class VsFn, class NextK, class NextV, class AddOdd>
+__device__ __forceinline__ void attend(Stage<C, D>& st, const Query<T, C, D>& q, State<D>& a, bool masked, bool partly, SeeFn see, LiveFn live, KsFn ks,
+                                       VsFn vs, NextK next_k, NextV next_v, AddOdd add_odd) {
   float s[2][4];
   float mx = kNegBig;
 #pragma unroll
@@ -376,6 +394,19 @@ __device__ __forceinline__ void attend(Stage<C, D>& st, const Query<T, C, D>& q,
           for (int w = 0; w < Stage<C, D>::kWords; ++w) st.v[4 * tl + i][w] = 0u;
         }
       }
+  }
+  bool found = false;
+  if (partly) {
+    unsigned any = 0u;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+      for (int w = 0; w < Stage<C, D>::kWords; ++w) {
+        const unsigned odd = C::odd(st.v[e][w]);
+        st.v[e][w] &= ~odd;
+        any |= odd;
+      }
+    found = __any(any != 0u);
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) mx = fmaxf(mx, fmaxf(s[0][i], s[1][i]));
@@ -429,6 +460,7 @@ __device__ __forceinline__ void attend(Stage<C, D>& st, const Query<T, C, D>& q,
   }
   next_v();
   PQC_LOADS_ISSUED();
+  if (found) add_odd();
 }
 
 __device__ __forceinline__ void store_out(const Geometry& g, void* out, size_t at, float x) {
@@ -684,6 +716,17 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(Geometry g, Cache c, 
   Query<T, C, D> qf;
   State<D> a;
   int lim = 0, least = 0;
+  auto add_odd = [&](int t, int buf) {
+    for (int tt = t; tt < min(t + kStep, now.most); ++tt) {
+      const int page = place[buf][at(now, tt)];
+      if (page < 0 || tt >= lim) continue;
+      const unsigned char* row = c.v + ((((size_t)page * g.Hkv + h) << g.shift) + (tt & (g.P - 1))) * row_bytes;
+#pragma unroll
+      for (int n = 0; n < D / 16; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a.o[n][i] += C::odd_value(row, D / 16 * (4 * quad + i) + n);
+    }
+  };
   look_up(now);
   if (threadIdx.x < 2) missing[threadIdx.x] = 0;
   __syncthreads();
@@ -719,7 +762,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(Geometry g, Cache c, 
       auto token = [&](int tl, int i) { return t + 16 * tl + 4 * quad + i; };
       auto slot = [&](int tl, int i) { return at(now, LISTED ? token(tl, i) : t + 16 * tl); };
       attend<T, C, D>(
-          st, qf, a, any_missing || t + kStep > least, [&](int tl, int i) { return token(tl, i) < lim && place[buf][slot(tl, i)] >= 0; },
+          st, qf, a, any_missing || t + kStep > least, !LISTED && g.R > 1 && t + kStep > least, [&](int tl, int i) { return token(tl, i) < lim && place[buf][slot(tl, i)] >= 0; },
           [&](int tl, int i) { return token(tl, i) < most && place[buf][slot(tl, i)] >= 0; }, [&](int tl, int i) { return kscale[slot(tl, i)]; },
           [&](int tl, int i) { return vscale[slot(tl, i)]; },
           [&]() {
@@ -727,7 +770,8 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(Geometry g, Cache c, 
           },
           [&]() {
             if (again) issue_v(now, buf, t + kGrain);
-          });
+          },
+          [&]() { add_odd(t, buf); });
     }
     if (more) put_places(next, buf ^ 1);
     lds_barrier();
@@ -881,6 +925,21 @@ struct BlockStage {
       }
     if (!v_ok) vs = 1.0f;
   }
+  // Takes values that are not finite out; true where a lane had some.
+  __device__ __forceinline__ bool clear_odd() {
+    unsigned any = 0u;
+    if ((threadIdx.x & 63) < kVLanes) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int i = 0; i < kV; ++i) {
+          const unsigned odd = C::odd(v[e][i]);
+          v[e][i] &= ~odd;
+          any |= odd;
+        }
+    }
+    return any != 0u;
+  }
   __device__ __forceinline__ void store_k(unsigned char* lk) const {
     const int tid = threadIdx.x, row = tid / 4, q = tid & 3;
     unsigned char* kr = lk + row * (D * 2);
@@ -973,6 +1032,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) void attn_
                                                             void* __restrict__ out, float* __restrict__ partials) {
   __shared__ __align__(16) unsigned char lds_k[2][kBlockTokens * D * 2], lds_v[2][kBlockTokens * D * 2];
   __shared__ unsigned present[2];  // a byte per 16 tokens of keys: their page is there
+  __shared__ int odd_values;       // of tokens that not all rows see some were not finite, and were taken out
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // the heads of a KV head's tokens follow each other, so that with eight of them an XCD's L2 holds the rows of one
   const int item = blockIdx.x / g.Hkv, h = blockIdx.x - item * g.Hkv;
@@ -1023,6 +1083,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) void attn_
     for (int i = 0; i < 16; ++i) o[n][i] = 0.0f;
   float m = kNegBig, l = 0.0f;
 
+  const int all_see = hidden + it.tile * g.R + 1;  // tokens that every row sees
+  if (tid == 0) odd_values = 0;
   const int t0 = it.split * it.tokens, t1 = it.n_split == 1 ? most : min(t0 + it.tokens, most);
   const int rounds = t0 < t1 ? (t1 - t0 + kBlockTokens - 1) / kBlockTokens : 0;
   const int mine = min(rounds, max(0, (wave_most - t0 + kBlockTokens - 1) / kBlockTokens));  // that the wave's rows see anything of
@@ -1046,6 +1108,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) void attn_
     };
     auto put_v = [&](int i) {
       if (!st.v_ok || wave_token(i) + 16 > most) st.clear_v(wave_token(i), most);
+      if (wave_token(i) + 16 > all_see && st.clear_odd()) odd_values = 1;
       st.store_v(lds_v[i & 1], wave);
     };
     constexpr int kAhead = 4;
@@ -1215,6 +1278,17 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) void attn_
         rescale();
 #pragma unroll
         for (int b = 0; b < 4; ++b) multiply(i, b >> 1, b & 1);
+      }
+    }
+    if (odd_values) {  // (set in front of the last barrier, if at all)
+      for (int t = t0 + max(all_see - t0, 0) / 16 * 16; t < min(t1, lim); ++t) {
+        const int page = table[t >> g.shift];
+        if (page < 0 || page >= g.n_pages) continue;
+        const unsigned char* row = c.v + ((((size_t)page * g.Hkv + h) << g.shift) + (t & (g.P - 1))) * (size_t)(D * C::kBytes);
+#pragma unroll
+        for (int n = 0; n < D / 32; ++n)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[n][e] += C::odd_value(row, 32 * n + 8 * (e >> 2) + 4 * half + (e & 3));
       }
     }
   }

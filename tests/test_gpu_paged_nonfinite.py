@@ -134,6 +134,26 @@ def test_a_value_that_is_not_a_number(paged, shape, cache, out):
     check(call, spoiled, shape)
 
 
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("shape,cache", [(s, c) for s in SHAPES if s.startswith(("rows", "block")) for c in ("fp8", "bf16")])
+def test_a_value_behind_a_query_is_not_its_own(paged, shape, cache, out, value):
+    # tokens that only some queries of a tile see: the others give them a weight of nothing, which must not meet the value
+    if cache == "fp8" and value == float("inf"):
+        pytest.skip("the type has no infinity")
+    call = Call(paged, shape, cache, out=out)
+    h, last = call.heads - 1, call.lengths[0] - 1
+    print(f"[case] {shape} {cache} {out} {value}", flush=True)
+    spoiled = torch.zeros((*call.q.shape[:2], 128), dtype=torch.bool)
+    for token, dim in ((last, 3), (last - 1, 64), (last - call.m + 3, 127), (last - call.m // 2, 70)):
+        call.spoil("v", 0, token, h, dim=dim, value=value)
+        spoiled |= call.seeing(0, token, h)[..., None] & (torch.arange(128) == dim)
+    want, tol = call.expected()
+    got = call.run().cpu()
+    assert not bool(torch.isfinite(got)[spoiled].any())
+    close(got, want.masked_fill(spoiled, float("nan")), tol, shape)
+
+
 # ------------------------------------------------------------------ append
 def is_nan_code(pages):
     return (pages.view(torch.uint8) & 0x7F) == 0x7F
