@@ -366,8 +366,10 @@ int pqc_block_cache_update(const pqc_config* cfg, int32_t block_tokens, int32_t 
  *
  *   k_pages, v_pages  [n_pages][Hkv][page_tokens][D]  cache_dtype
  *   k_scale, v_scale  [n_pages][Hkv] f32   PQC_FP8 only (else ignored, may be NULL): a row's
- *                                          values are code * scale of its page and head, a
- *                                          power of two (as pqc_paged_append leaves it)
+ *                                          values are code * scale of its page and head;
+ *                                          pqc_paged_append leaves powers of two, pools that
+ *                                          were filled elsewhere may have any positive normal
+ *                                          numbers
  *   page_table        [B][max_pages] int32 pages of sequence b; an entry outside
  *                                          [0, n_pages) is a page that is not there: nothing
  *                                          is written to it and none of its tokens attended

@@ -982,6 +982,12 @@ struct BlockStage {
   }
 };
 
+// The conversion of codes takes a scale's power of two alone.  Of its bits: what there is beside (a sign or a significand), and that as a factor.
+__device__ __forceinline__ unsigned beside_power(unsigned scale) { return scale & 0x807fffffu; }
+__device__ __forceinline__ float rest_of_scale(unsigned scale) {
+  return __uint_as_float((scale & 0x7f800000u) == 0x7f800000u ? 0x7fc00000u : beside_power(scale) | 0x3f800000u);
+}
+
 // Folds the splits of the tiles of the kernel below: many rows, few splits.
 template <int D>
 __global__ __launch_bounds__(256) void attn_block_fold_kernel(Geometry g, const int* __restrict__ lengths, const int* __restrict__ offsets,
@@ -1031,7 +1037,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) void attn_
                                                                                             const int* __restrict__ offsets,
                                                             void* __restrict__ out, float* __restrict__ partials) {
   __shared__ __align__(16) unsigned char lds_k[2][kBlockTokens * D * 2], lds_v[2][kBlockTokens * D * 2];
-  __shared__ unsigned present[2];  // a byte per 16 tokens of keys: their page is there
+  // A byte per 16 tokens of keys: their page is there (1), its scale is no power of two (2), nor that of the values one round earlier (4); and
+  // what those scales are beside their powers of two.
+  __shared__ unsigned present[2];
+  __shared__ float k_rest[2][4], v_rest[2][4];
   __shared__ int odd_values;       // of tokens that not all rows see some were not finite, and were taken out
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // the heads of a KV head's tokens follow each other, so that with eight of them an XCD's L2 holds the rows of one
@@ -1101,15 +1110,28 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) void attn_
       return p < g.n_pages ? p : -1;
     };
     auto wave_token = [&](int i) { return t0 + i * kBlockTokens + 16 * wave; };
-    auto put_k = [&](int i) {
-      if (!st.k_ok || wave_token(i) + 16 > most) st.clear_k(wave_token(i), most);
-      st.store_k(lds_k[i & 1]);
-      if (lane == 0) reinterpret_cast<unsigned char*>(&present[i & 1])[wave] = (unsigned char)st.k_ok;
-    };
     auto put_v = [&](int i) {
       if (!st.v_ok || wave_token(i) + 16 > most) st.clear_v(wave_token(i), most);
       if (wave_token(i) + 16 > all_see && st.clear_odd()) odd_values = 1;
       st.store_v(lds_v[i & 1], wave);
+    };
+    // keys of round i and values of round i - 1
+    auto put = [&](int i, bool values) {
+      if (!st.k_ok || wave_token(i) + 16 > most) st.clear_k(wave_token(i), most);
+      st.store_k(lds_k[i & 1]);
+      if (values) put_v(i - 1);
+      unsigned flags = st.k_ok ? 1u : 0u;
+      if constexpr (C::kBytes == 1) {
+        const unsigned ks = __float_as_uint(st.ks), vs = __float_as_uint(st.vs);
+        if (__builtin_amdgcn_readfirstlane(beside_power(ks | vs))) {
+          flags |= (beside_power(ks) ? 2u : 0u) | (beside_power(vs) ? 4u : 0u);
+          if (lane == 0) {
+            k_rest[i & 1][wave] = rest_of_scale(ks);
+            v_rest[(i & 1) ^ 1][wave] = rest_of_scale(vs);
+          }
+        }
+      }
+      if (lane == 0) reinterpret_cast<unsigned char*>(&present[i & 1])[wave] = (unsigned char)flags;
     };
     constexpr int kAhead = 4;
     f32x16_t s[2];
@@ -1146,10 +1168,26 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) void attn_
       }
       __builtin_amdgcn_sched_group_barrier(0x008, kQ * kAhead, 0);
     };
+    auto flags_of = [&](int i) { return (unsigned)__builtin_amdgcn_readfirstlane(present[i & 1]); };
+    // weights of round i by what the scales of its values are beside their powers of two
+    auto scale_weights = [&](int i, unsigned there) {
+      if (C::kBytes == 1 && (there & 0x04040404u)) {
+#pragma unroll
+        for (int e = 0; e < 32; ++e)
+          if ((there >> (8 * (e >> 3))) & 4u) w[e] *= v_rest[i & 1][e >> 3];
+      }
+    };
+    // logits of round i, and weights of the round before: all that is not the same for most rounds, behind one branch
     auto mask = [&](int i) {
       const int t = t0 + i * kBlockTokens;
-      const unsigned there = __builtin_amdgcn_readfirstlane(present[i & 1]);
+      const unsigned there = flags_of(i);
       if (t + kBlockTokens > least || there != 0x01010101u) {
+        if (C::kBytes == 1 && (there & 0x02020202u)) {
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+            if ((there >> (8 * (e >> 3))) & 2u) s[e >> 4][e & 15] *= k_rest[i & 1][e >> 3];
+        }
+        if (i > 0) scale_weights(i - 1, there);
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -1223,7 +1261,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) void attn_
       st.load_k(g, c, h, wave_token(0), page0);
       st.load_v(g, c, h, wave_token(0), page0);
     }
-    put_k(0);
+    put(0, false);
     st.load_k(g, c, h, wave_token(1), page1);
     __syncthreads();
     if (mine > 0) {
@@ -1234,13 +1272,11 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) void attn_
 #pragma unroll
       for (int b = 0; b < 4; ++b) weigh(b >> 1, b & 1);
     }
-    put_k(1);
-    put_v(0);
+    put(1, true);
     st.load_k(g, c, h, wave_token(2), page2);
     st.load_v(g, c, h, wave_token(1), page1);
     auto stage = [&](int i) {
-      put_k(i + 2);
-      put_v(i + 1);
+      put(i + 2, true);
       const int next = valid(page3);
       st.load_k(g, c, h, wave_token(i + 3), next);
       st.load_v(g, c, h, wave_token(i + 2), page2);
@@ -1275,6 +1311,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) void attn_
       __syncthreads();
       if (i + 1 < rounds) stage(i);
       if (i < mine) {
+        scale_weights(i, flags_of(i + 1));
         rescale();
 #pragma unroll
         for (int b = 0; b < 4; ++b) multiply(i, b >> 1, b & 1);

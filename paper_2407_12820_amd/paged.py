@@ -99,8 +99,8 @@ def rotation_table(n_positions: int, rot_dims: int, base: float = 10000.0, devic
 # The small calls are shorter than what Python does in front of them, so that each tensor is checked in one expression on the
 # quickest of torch's accessors, and what is wrong is worked out by _need and _rows only if something is.
 class PagedCache:
-    """Pages [n_pages][Hkv][page_tokens][D] of keys and of values, float8_e4m3fn with scales [n_pages][Hkv] f32, or bfloat16
-    (scales None).  `dtype`: "f32" or "bf16", of q, k and v; `out_dtype`: of the attention output; `rotation`: the table of
+    """Pages [n_pages][Hkv][page_tokens][D] of keys and of values, float8_e4m3fn with scales [n_pages][Hkv] f32 (positive; `append` leaves
+    powers of two), or bfloat16 (scales None).  `dtype`: "f32" or "bf16", of q, k and v; `out_dtype`: of the attention output; `rotation`: the table of
     rotation_table() or one laid out like it, None for no rotation.  Like a decode context it is not thread-safe.
 
     Calls run on the current stream, or on `stream`, to which their allocations then belong too.  They may be recorded into
