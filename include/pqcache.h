@@ -429,8 +429,8 @@ typedef struct pqc_paged_cache { /* device pointers, 16-byte aligned (page_table
  *   positions  [n] int32   row of the table for each token, taken into it; NULL: the token's
  *                          place in its sequence
  *   q_out      [n][Hq][D]  rotated queries (required with q), k_out [n][Hkv][D] rotated keys
- *                          (may be NULL; for pqc_pq_build, pqc_pq_encode_token): io_dtype,
- *                          not overlapping the inputs
+ *                          (may be NULL; for pqc_pq_build, pqc_pq_encode_token): io_dtype;
+ *                          over each other, an input or the pools: PQC_EINVAL
  * A token goes to place lengths[b] - (tokens of b) + i of its sequence; places outside
  * [0, max_pages * page_tokens) are not stored.  A page written to must be named once
  * in the table.
@@ -462,7 +462,8 @@ size_t pqc_paged_counter_bytes(const pqc_paged_config* cfg);
  * t <= lengths[b] - m + i.  A query that sees none gives zeros; tokens that it does not see leave it
  * alone, whatever they hold (NaN and infinities included).  Sequences with one query token and
  * sequences with many are quicker in calls of their own.
- *   q    [n][Hq][D] io_dtype     out  [n][Hq][D] out_dtype, not overlapping the inputs
+ *   q    [n][Hq][D] io_dtype     out  [n][Hq][D] out_dtype (over an input, the pools or the
+ *                                     workspace: PQC_EINVAL)
  *   workspace  256-byte aligned, pqc_paged_workspace_bytes(cfg, n, 0); contents need not be
  *              kept, calls that share it must be ordered on one stream
  * Sums, maxima and softmax weights are fp32; weights enter the product with the values whole, or, for

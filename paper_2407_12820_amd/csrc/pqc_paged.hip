@@ -13,6 +13,28 @@ using namespace pqc::paged;
 
 bool aligned(const void* p, unsigned n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
+// Rows of `row` bytes, `stride` bytes apart.
+struct Rows {
+  const void* at;
+  long long n, row, stride;
+};
+Rows bytes_at(const void* p, long long bytes) { return Rows{p, 1, bytes, bytes}; }
+// Whether any byte of [p, p + bytes) is one of theirs: the first row that ends behind p begins in front of the end, or none does.
+bool meets(const void* p, long long bytes, const Rows& r) {
+  if (!p || !r.at || bytes <= 0 || r.n <= 0 || r.row <= 0) return false;
+  const long long from = (long long)reinterpret_cast<uintptr_t>(p) - (long long)reinterpret_cast<uintptr_t>(r.at);  // p as seen from the first row
+  if (from < r.row) return from + bytes > 0;
+  if (r.n == 1) return false;
+  const long long i = (from - r.row) / r.stride + 1;
+  return i < r.n && i * r.stride < from + bytes;
+}
+template <size_t N>
+bool meets_any(const void* p, long long bytes, const Rows (&rows)[N]) {
+  for (const Rows& r : rows)
+    if (meets(p, bytes, r)) return true;
+  return false;
+}
+
 // A launch takes fewer than 2^32 work items, workgroups have 256.
 constexpr long long kMaxGroups = 1ll << 24;
 
@@ -125,6 +147,21 @@ int check_cache(const pqc_paged_config* cfg, const pqc_paged_cache* c) {
   if (cfg->cache_dtype == PQC_FP8 && (!aligned(c->k_scale, 16) || !aligned(c->v_scale, 16))) return PQC_EINVAL;
   return PQC_OK;
 }
+// Outputs in the pools, or over what says where things lie.
+bool over_cache(const void* p, long long bytes, const pqc_paged_config* cfg, const pqc_paged_cache* c) {
+  const long long rows = (long long)cfg->n_pages * cfg->n_kv_heads, pool = rows * cfg->page_tokens * cfg->head_dim * (cfg->cache_dtype == PQC_FP8 ? 1 : 2);
+  const long long scales = cfg->cache_dtype == PQC_FP8 ? rows * 4 : 0;
+  return meets_any(p, bytes, {bytes_at(c->k_pages, pool), bytes_at(c->v_pages, pool), bytes_at(c->k_scale, scales), bytes_at(c->v_scale, scales),
+                              bytes_at(c->page_table, (long long)cfg->batch * cfg->max_pages * 4), bytes_at(c->lengths, cfg->batch * 4ll)});
+}
+// An attention call's output over what it reads or keeps its parts in.
+bool out_overlaps(const pqc_paged_config* cfg, const pqc_paged_cache* c, const void* q, long long n, const int* offsets, const int* idx, long long n_idx,
+                  const void* out, const void* workspace, long long workspace_bytes) {
+  const long long values = n * cfg->n_q_heads * cfg->head_dim, bytes = values * (cfg->out_dtype == PQC_F32 ? 4 : 2);
+  return over_cache(out, bytes, cfg, c) ||
+         meets_any(out, bytes, {bytes_at(q, values * (cfg->io_dtype == PQC_F32 ? 4 : 2)), bytes_at(offsets, (cfg->batch + 1) * 4ll),
+                                bytes_at(idx, (long long)cfg->batch * cfg->n_kv_heads * n_idx * 4), bytes_at(workspace, workspace_bytes)});
+}
 Cache device_cache(const pqc_paged_cache* c) {
   return Cache{static_cast<unsigned char*>(c->k_pages), static_cast<unsigned char*>(c->v_pages), c->k_scale, c->v_scale, c->page_table, c->lengths, c->counters};
 }
@@ -236,6 +273,7 @@ int pqc_paged_attn(const pqc_paged_config* cfg, const pqc_paged_cache* cache, co
   if ((long long)g.items * g.Hkv >= kMaxGroups) return PQC_EUNSUPPORTED;
   if (!workspace || !aligned(workspace, 256) || workspace_bytes < need) return PQC_EWORKSPACE;
   if (n == 0) return PQC_OK;
+  if (out_overlaps(cfg, cache, q, n, offsets, nullptr, 0, out, workspace, (long long)need)) return PQC_EINVAL;
   const Cache c = device_cache(cache);
   const AttnCall call{g, c, q, offsets, nullptr, 0, out, static_cast<float*>(workspace), static_cast<hipStream_t>(stream)};
   return form == Tiles::kBlock ? launch_blocks(cfg, call) : launch_attn<false>(cfg, call);
@@ -253,6 +291,7 @@ int pqc_paged_gather_attn(const pqc_paged_config* cfg, const pqc_paged_cache* ca
   plan_listed(&g, n_idx);
   const size_t need = partial_bytes(g, cfg->head_dim);
   if (need && (!workspace || !aligned(workspace, 256) || workspace_bytes < need)) return PQC_EWORKSPACE;
+  if (out_overlaps(cfg, cache, q, g.B, nullptr, idx, n_idx, out, workspace, (long long)need)) return PQC_EINVAL;
   const Cache c = device_cache(cache);
   return launch_attn<true>(cfg, AttnCall{g, c, q, nullptr, idx, n_idx, out, static_cast<float*>(workspace), static_cast<hipStream_t>(stream)});
 }
@@ -271,8 +310,6 @@ int pqc_paged_append(const pqc_paged_config* cfg, const pqc_paged_cache* cache, 
       !aligned(offsets, 4) || !aligned(positions, 4))
     return PQC_EINVAL;
   if (k_stride < kv_row || v_stride < kv_row || k_stride % 8 || v_stride % 8 || (q && (q_stride < q_row || q_stride % 8))) return PQC_EINVAL;
-  // a value's partner may be read after it was overwritten
-  if ((q && q_out == q) || (k_out && (k_out == k || k_out == v || k_out == q || k_out == q_out))) return PQC_EINVAL;
   if (n == 0) return PQC_OK;
   AppendArgs a;
   a.q = q; a.k = k; a.v = v;
@@ -291,6 +328,14 @@ int pqc_paged_append(const pqc_paged_config* cfg, const pqc_paged_cache* cache, 
   pages = (pages + a.together - 1) / a.together * a.together;
   if (pages * 2 * g.Hkv + (q ? (n + a.q_tokens - 1) / a.q_tokens : 0) >= kMaxGroups) return PQC_EUNSUPPORTED;
   a.kv_items = (int)pages;
+  // other workgroups may read an input after a workgroup has stored its part of an output
+  const int e = cfg->io_dtype == PQC_F32 ? 4 : 2;
+  const Rows in[] = {{q, n, q_row * e, q_stride * e}, {k, n, kv_row * e, k_stride * e}, {v, n, kv_row * e, v_stride * e}, bytes_at(offsets, (g.B + 1) * 4ll),
+                     bytes_at(positions, n * 4ll), bytes_at(rotation, (long long)cfg->rot_positions * cfg->rot_dims * 4)};
+  const long long q_bytes = q ? n * q_row * e : 0, k_bytes = n * kv_row * e;
+  if (meets_any(q_out, q_bytes, in) || meets_any(k_out, k_bytes, in) || meets(k_out, k_bytes, bytes_at(q_out, q_bytes)) || over_cache(q_out, q_bytes, cfg, cache) ||
+      over_cache(k_out, k_bytes, cfg, cache))
+    return PQC_EINVAL;
   const Cache c = device_cache(cache);
   hipStream_t st = static_cast<hipStream_t>(stream);
   auto by_dim = [&](auto t, auto fp8) {

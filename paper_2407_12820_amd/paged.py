@@ -129,6 +129,7 @@ class PagedCache:
             self._need(rotation, torch.float32, rotation.shape, "rotation")
         self._rotation = None if rotation is None else rotation.data_ptr()
         self.heads, self.dim, self.q_heads = heads, dim, n_q_heads
+        self._q_row, self._out_row = n_q_heads * dim * self.io.itemsize, n_q_heads * dim * self.out.itemsize  # bytes of a token
         self.cfg = Config(1, n_q_heads, heads, dim, tokens, n_pages, 1, _DTYPES[dtype][0], 2 if fp8 else 1, _DTYPES[out_dtype][0],
                           softmax_scale, rot_dims, _STYLES[rot_style], rot_positions)
         self.pages = Pages(k_pages.data_ptr(), v_pages.data_ptr(), k_scale.data_ptr() if fp8 else None,
@@ -289,7 +290,7 @@ class PagedCache:
         if out is None:
             out = torch.empty((n, self.q_heads, self.dim), dtype=self.out, device=self.device)
         op = self._plain(out, self.out, n, self.q_heads, "out")
-        if op == qp and n:
+        if op < qp + n * self._q_row and qp < op + n * self._out_row:
             raise ValueError("out must not overlap q")
         if n:
             self._attend("pqc_paged_attn", self.lib.pqc_paged_attn, n, 0, (self._cfg, self._pages, qp, n, off, op))
@@ -310,7 +311,7 @@ class PagedCache:
         if out is None:
             out = torch.empty((b, self.q_heads, self.dim), dtype=self.out, device=self.device)
         op = self._plain(out, self.out, b, self.q_heads, "out")
-        if op == qp and b:
+        if op < qp + b * self._q_row and qp < op + b * self._out_row:
             raise ValueError("out must not overlap q")
         self._attend("pqc_paged_gather_attn", self.lib.pqc_paged_gather_attn, b, n_idx, (self._cfg, self._pages, qp, idx.data_ptr(), n_idx, op))
         return out
