@@ -4,8 +4,8 @@ A `PagedCache` is a view of a pool of pages that the caller owns: which sequence
 call as a page table and lengths, so that one object serves a batch that changes from step to step.
 
 Scratch memory of the attention calls: one workspace and one block of counters per stream, which all caches share, since
-what runs on a stream runs in order.  A call that is recorded into a graph has a workspace out of the graph's own memory and
-counters that no other call gets, so that two graphs share none.
+what runs on a stream runs in order.  A call that is recorded into a graph has a workspace out of the graph's own memory, and
+counters that only the calls recorded on the same stream into the same graph get, so that two graphs share none.
 """
 from __future__ import annotations
 
@@ -50,6 +50,8 @@ def _load():
         lib.pqc_paged_attn.argtypes = [cfg, pages, vp, i32, vp, vp, vp, size, vp]
         lib.pqc_paged_gather_attn.restype = C.c_int
         lib.pqc_paged_gather_attn.argtypes = [cfg, pages, vp, vp, i32, vp, vp, size, vp]
+        lib.hipStreamGetCaptureInfo.restype = C.c_int  # of the HIP runtime that the library is linked to
+        lib.hipStreamGetCaptureInfo.argtypes = [vp, C.POINTER(C.c_int), C.POINTER(C.c_uint64)]
         _lib = lib
     return _lib
 
@@ -68,21 +70,34 @@ class _Scratch:
 
 
 class _Device:
-    """Scratch memory of a GPU: by raw stream, and counters for recorded calls."""
+    """Scratch memory of a GPU: by raw stream, and counters for recordings."""
 
-    RECORDED = 64  # recorded calls that get counters of their own; later ones take a launch more
+    SPARE = 64     # blocks of counters that are made at a time; a recording without one takes a launch more
     WORDS = 512    # counters that a call of up to 512 KV heads needs
 
     def __init__(self):
-        self.streams, self.spare, self.recorded = {}, [], []
+        self.streams, self.spare = {}, []
+        self.recorded = {}  # by recording and raw stream: its graph's for good, 2 KB each
 
     def stream(self, raw: int, device) -> _Scratch:
+        """For a call that runs now, which also sees to counters for the recordings to come."""
+        if not self.spare:
+            self.spare = list(torch.zeros((self.SPARE, self.WORDS), dtype=torch.int32, device=device))
+            torch.cuda.current_stream(device).synchronize()  # a graph may run on any stream
         found = self.streams.get(raw)
         if found is None:
-            if not self.streams:
-                self.spare = list(torch.zeros((self.RECORDED, self.WORDS), dtype=torch.int32, device=device))
             found = self.streams[raw] = _Scratch(device, self.WORDS)
         return found
+
+    def recording(self, raw: int, lib) -> Optional[torch.Tensor]:
+        """Counters for a call that is being recorded on this stream; None: there are none left."""
+        status, at = C.c_int(0), C.c_uint64(0)
+        if lib.hipStreamGetCaptureInfo(raw, C.byref(status), C.byref(at)) != 0:
+            return None
+        key = at.value, raw
+        if key not in self.recorded and self.spare:
+            self.recorded[key] = self.spare.pop()
+        return self.recorded.get(key)
 
 
 _devices = {}
@@ -223,14 +238,13 @@ class PagedCache:
     def _launch(self, what: str, fn, need: int, args) -> None:
         raw = torch._C._cuda_getCurrentRawStream(self._dev)
         if torch._C._cuda_isCurrentStreamCapturing():
-            own = self._scratch.spare.pop() if self._scratch.spare and self._counted else None
-            self._scratch.recorded.append(own)  # the graph's for good
+            own = self._scratch.recording(raw, self.lib) if self._counted else None
             counters = None if own is None else own.data_ptr()
             workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
             at, size = workspace.data_ptr(), need
         else:
             scratch = self._scratch.streams.get(raw)
-            if scratch is None:
+            if scratch is None or not self._scratch.spare:
                 scratch = self._scratch.stream(raw, self.device)
             if scratch.size < need:
                 scratch.grow(need)
