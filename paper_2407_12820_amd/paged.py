@@ -327,5 +327,6 @@ class PagedCache:
         op = self._plain(out, self.out, b, self.q_heads, "out")
         if op < qp + b * self._q_row and qp < op + b * self._out_row:
             raise ValueError("out must not overlap q")
-        self._attend("pqc_paged_gather_attn", self.lib.pqc_paged_gather_attn, b, n_idx, (self._cfg, self._pages, qp, idx.data_ptr(), n_idx, op))
+        if b:
+            self._attend("pqc_paged_gather_attn", self.lib.pqc_paged_gather_attn, b, n_idx, (self._cfg, self._pages, qp, idx.data_ptr(), n_idx, op))
         return out
