@@ -134,13 +134,11 @@ def test_a_value_that_is_not_a_number(paged, shape, cache, out):
     check(call, spoiled, shape)
 
 
-@pytest.mark.parametrize("value", [float("nan"), float("inf")])
 @pytest.mark.parametrize("out", ["f32", "bf16"])
-@pytest.mark.parametrize("shape,cache", [(s, c) for s in SHAPES if s.startswith(("rows", "block")) for c in ("fp8", "bf16")])
-def test_a_value_behind_a_query_is_not_its_own(paged, shape, cache, out, value):
+@pytest.mark.parametrize("cache,value", [("fp8", float("nan")), ("bf16", float("nan")), ("bf16", float("inf"))])
+@pytest.mark.parametrize("shape", [s for s in SHAPES if s.startswith(("rows", "block"))])
+def test_a_value_behind_a_query_is_not_its_own(paged, shape, cache, value, out):
     # tokens that only some queries of a tile see: the others give them a weight of nothing, which must not meet the value
-    if cache == "fp8" and value == float("inf"):
-        pytest.skip("the type has no infinity")
     call = Call(paged, shape, cache, out=out)
     h, last = call.heads - 1, call.lengths[0] - 1
     print(f"[case] {shape} {cache} {out} {value}", flush=True)
