@@ -17,6 +17,7 @@ constexpr int kStep = 32;          // tokens that a wave takes at a time
 constexpr int kWaves = 4;
 constexpr int kGrain = kWaves * kStep;  // tokens of a split are a multiple of this
 constexpr int kStaged = 512;       // pages (or listed tokens) whose place and scales lie in LDS at a time
+constexpr float kLowest = -3.402823466e38f;  // maximum of the logits of a row that has seen nothing: no finite logit is below it
 constexpr float kFp8Max = 448.0f;  // largest e4m3 value, 0.875 * 2^9
 
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
@@ -351,7 +352,7 @@ struct State {
   __device__ __forceinline__ void init() {
 #pragma unroll
     for (int n = 0; n < D / 16; ++n) o[n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    m = kNegBig;
+    m = kLowest;
     l = 0.0f;
   }
 };
@@ -368,7 +369,7 @@ template <typename T, class C, int D, class SeeFn, class LiveFn, class KsFn, cla
 __device__ __forceinline__ void attend(Stage<C, D>& st, const Query<T, C, D>& q, State<D>& a, bool masked, bool partly, SeeFn see, LiveFn live, KsFn ks,
                                        VsFn vs, NextK next_k, NextV next_v, AddOdd add_odd) {
   float s[2][4];
-  float mx = kNegBig;
+  float mx = kLowest;
 #pragma unroll
   for (int tl = 0; tl < 2; ++tl) {
     f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
@@ -507,7 +508,7 @@ __device__ __forceinline__ void fold_parts(const Geometry& g, const Seq& s, int 
     const int r = r0 + group / sides, qr = tile * g.R + r / g.G;
     const bool live = r < row1 && qr < s.nq;
     f32x4_t o = {0.f, 0.f, 0.f, 0.f};
-    float m = kNegBig, l = 0.0f;
+    float m = kLowest, l = 0.0f;
     if (live) {
       for (int i = side; i < n; i += kAhead * sides) {
         float2 ml[kAhead];
@@ -1001,7 +1002,7 @@ __global__ __launch_bounds__(256) void attn_block_fold_kernel(Geometry g, const 
   for (int r = blockIdx.z * kAtOnce + threadIdx.x / kLanes; r < rows; r += gridDim.z * kAtOnce) {
     const int qr = it.tile * g.R + r / g.G;
     if (qr >= it.s.nq) return;
-    float m = kNegBig, l = 0.0f;
+    float m = kLowest, l = 0.0f;
     f32x4_t o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
     for (int i = 0; i < it.n_split; ++i) {
@@ -1090,7 +1091,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) void attn_
   for (int n = 0; n < D / 32; ++n)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[n][i] = 0.0f;
-  float m = kNegBig, l = 0.0f;
+  float m = kLowest, l = 0.0f;
 
   const int all_see = hidden + it.tile * g.R + 1;  // tokens that every row sees
   if (tid == 0) odd_values = 0;
@@ -1198,29 +1199,42 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) void attn_
       }
     };
     // Exponents of the weights, relative to m (to 0 as long as the row has seen nothing).  Weights may reach 2^8 before a larger
-    // maximum is taken: O and l are relative to the same.
+    // maximum is taken: O and l are relative to the same.  Product and difference are one rounding, but for maxima beyond 2^24 (`far`), whose own
+    // rounding would then count as a weight, of up to infinity: there the product is rounded as the maximum was.
+    bool far = false;
     auto raise = [&](float& corr) {
+      float factor = g.scale_log2e;
+      if (far) {
+#pragma clang fp contract(off)
+        factor = 1.0f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          s[0][e] *= g.scale_log2e;
+          s[1][e] *= g.scale_log2e;
+        }
+      }
       float mx = -INFINITY;
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        s[0][e] = fmaf(s[0][e], g.scale_log2e, -reference);
-        s[1][e] = fmaf(s[1][e], g.scale_log2e, -reference);
+        s[0][e] = fmaf(s[0][e], factor, -reference);
+        s[1][e] = fmaf(s[1][e], factor, -reference);
         mx = fmaxf(mx, fmaxf(s[0][e], s[1][e]));
       }
       const u32x2_t both = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
       mx = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) + reference;
       const bool up = __any(mx > m + 8.0f);
       if (up) {
-        const float mnew = fmaxf(m, mx);
+        const float mnew = fmaxf(m, mx), before = reference;
         corr = __builtin_amdgcn_exp2f(m - mnew);
         m = mnew;
         l *= corr;
-        const float ref = m > 0.5f * kNegBig ? m : 0.0f, by = ref - reference;
-        reference = ref;
+        reference = m > kLowest ? m : 0.0f;
+        far = __any(fabsf(reference) > 0x1p24f);
+        const float back = far ? before : 0.0f, by = far ? reference : reference - before;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          s[0][e] -= by;
-          s[1][e] -= by;
+          s[0][e] = (s[0][e] + back) - by;
+          s[1][e] = (s[1][e] + back) - by;
         }
       }
       return up;

@@ -208,3 +208,28 @@ def test_a_page_that_begins_with_an_infinity(paged):
     assert float(c.k_scale) == s and bool(is_nan_code(c.k_pages)[0, 0, 0].all())
     got = ref.dequantised(c.k_pages.cpu(), c.k_scale.cpu())[0, 0, 1:3]
     assert bool(((got - x[:, 0].double()).abs() <= 2.0 ** -4 * x[:, 0].double().abs() + 2.0 ** -9 * s).all())
+
+
+# ------------------------------------------------------------------ logits of any size
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_logits_of_any_finite_size(paged, shape, dtype, sign):
+    """Logits of 2^30 to 2^110, all of one sign: the softmax is that of equal or far apart numbers, never of masked ones."""
+    call = Call(paged, shape, "bf16", dtype)
+    call.q[:] = 0.0
+    call.q[..., 3] = 1.3359375 * torch.exp2(torch.randint(-20, 61, call.q.shape[:2], generator=call.gen).float())
+    h, best = call.heads - 1, call.lengths[0] // 3
+    if call.idx is not None:
+        best = int(call.idx[0, h, 11])
+    print(f"[case] {shape} {dtype} {sign}", flush=True)
+    k = call.pages[0]
+    k[...] = 0.0
+    k[..., 3] = sign * 1.6328125 * 2.0 ** 53
+    # one head of the first sequence has a token far ahead of the others, the rest equal logits
+    k[int(call.table[0, best // 64]), h, best % 64, 3] = sign * 2.0 ** 54 * (1.5 if sign > 0 else 0.5)
+    call.c.k_pages.copy_(k)
+    want, _ = call.expected()
+    got = call.run().double().cpu()
+    # every product and every logit is exact or equal to its like, weights are 1 or 0: what is left are the sums (values of up to 5 in size)
+    assert (got - want).abs().max().item() <= 5 * (max(call.lengths) / 4 + 64) * ref.U
