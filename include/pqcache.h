@@ -374,8 +374,8 @@ int pqc_block_cache_update(const pqc_config* cfg, int32_t block_tokens, int32_t 
  *                                          [0, n_pages) is a page that is not there: nothing
  *                                          is written to it and none of its tokens attended
  *   lengths           [B] int32            tokens of each sequence, the ones that a call
- *                                          appends or queries with included; taken into
- *                                          [0, max_pages * page_tokens]
+ *                                          appends or queries with included; attention takes
+ *                                          them into [0, max_pages * page_tokens]
  *
  * The calls need no context, allocate nothing and synchronise nothing; the lengths, offsets
  * and page tables are read on the device, so that a call recorded into a HIP graph follows
@@ -426,19 +426,21 @@ typedef struct pqc_paged_cache { /* device pointers, 16-byte aligned (page_table
  *       three may be parts of the rows of one projection).  q may be NULL.
  *   rotation   [rot_positions][rot_dims] f32   per position cos of the rot_dims/2 angles, then
  *                                              sin; NULL with rot_dims == 0
- *   positions  [n] int32   row of the table for each token, taken into it; NULL: the token's
- *                          place in its sequence
+ *   positions  [n] int32   row of the table for each token; NULL: the token's place in its
+ *                          sequence.  Either is taken into [0, rot_positions): a table shorter
+ *                          than the sequences turns all tokens behind it by its last row
  *   q_out      [n][Hq][D]  rotated queries (required with q), k_out [n][Hkv][D] rotated keys
  *                          (may be NULL; for pqc_pq_build, pqc_pq_encode_token): io_dtype;
  *                          over each other, an input or the pools: PQC_EINVAL
  * A token goes to place lengths[b] - (tokens of b) + i of its sequence; places outside
- * [0, max_pages * page_tokens) are not stored.  A page written to must be named once
- * in the table.
+ * [0, max_pages * page_tokens) are not stored, and their rows of k_out keep what they held (those
+ * of q_out are written).  A page written to must be named once in the table.
  * PQC_FP8: the scale of a (page, head), of keys and of values apart, is the smallest power of two
  * (2^-100 at least) with which all its finite values are within the type's 448; a value that is
  * infinite or not a number is stored as the type's NaN.  If a page's scale has to grow for new
  * tokens, its older codes are encoded anew, which a power of two leaves exact down to the
- * type's subnormals.  A page that receives its first token starts anew, whatever it held. */
+ * type's subnormals.  Tokens taken back (by a shorter length) leave the scale that they needed.  A
+ * page that receives its first token starts anew, whatever it held. */
 int pqc_paged_append(const pqc_paged_config* cfg, const pqc_paged_cache* cache, const void* q, int64_t q_stride,
                      const void* k, int64_t k_stride, const void* v, int64_t v_stride, int32_t n,
                      const int32_t* offsets, const int32_t* positions, const float* rotation, void* q_out,
@@ -446,7 +448,8 @@ int pqc_paged_append(const pqc_paged_config* cfg, const pqc_paged_cache* cache, 
 
 /* Bytes of device workspace of the two attention calls below, for n query tokens over all
  * sequences and, for pqc_paged_gather_attn, n_idx listed tokens per head (0 for
- * pqc_paged_attn).  Of the configuration's sizes alone, not of what the arrays hold.  0 if the
+ * pqc_paged_attn).  Of the configuration's sizes alone, not of what the arrays hold, and for calls
+ * with offsets and without: the larger of the two.  0 if the
  * configuration is refused, and where no workspace is needed. */
 size_t pqc_paged_workspace_bytes(const pqc_paged_config* cfg, int32_t n, int32_t n_idx);
 

@@ -52,7 +52,8 @@ constexpr int kWorkers = 512;
 constexpr size_t kRowsLds = 56 * 1024;
 // One per compute unit where there is little to do for each: twice as many have as many more parts to fold.  us with 512 and 256, 8 heads of 4
 // query heads, one sequence of 4096 tokens 13.4, 12.8, 6144 15.6, 13.5, 16384 19.5, 18.0, 32768 23.5, 23.5, two of 4096 17.1, 14.4; listed, 4096
-// tokens 13.0, 12.0, 6600 14.6, 13.1, 13175 16.4, 15.4.
+// tokens 13.0, 12.0, 6600 14.6, 13.1, 13175 16.4, 15.4.  (This rule and kPartsFolded go by the width of the page table, since the lengths are known
+// on the device alone: short sequences under a wide table are planned as long ones.)
 constexpr int kFewUnits = 4;
 // Items of the kernel of 128 rows that the length of a split aims at.
 constexpr int kBlockItems = 480;
@@ -95,9 +96,10 @@ int make_geometry(const pqc_paged_config* c, long long n, Geometry* g) {
 }
 
 // What takes a call: a tile per query token, tiles of 16 rows, or (many queries per sequence) of 128 rows.
-// Tiles of 128 rows from 64 rows per sequence on (8 heads of 4 query heads; us with tiles of 16 and of 128: one sequence of 17482 tokens, 32
-// rows 33.1, 38.3, 64 40.1, 38.5, 96 49.8, 40.1, 256 85.6, 45.5; sixteen of 4096, 32 rows 48.7, 49.3, 64 70.7, 53.9).  Their splits are of
-// 512 tokens at least, since each leaves up to 64 KB of partial results (512 queries on themselves: splits of 256 26.8, of 512 19.0).
+// Tiles of 128 rows from 64 rows per sequence on, which is the average: single tokens among prompts take a tile each (8 heads of 4 query heads, bf16
+// output; us with tiles of 16 and of 128: one sequence of 17482 tokens, 32 rows 31.5, 42.4, 64 40.1, 42.9, 96 49.6, 44.3, 256 85.7, 51.6; sixteen
+// of 4096, 32 rows 48.3, 58.1, 64 70.8, 62.4; with an fp32 output, one more product, 64 rows 40.1, 47.5 and 70.7, 75.1, 256 85.7, 57.4).  Their
+// splits are of 512 tokens at least, since each leaves up to 64 KB of partial results (512 queries on themselves: splits of 256 28.8, of 512 22.3).
 enum class Tiles { kOne, kRows, kBlock };
 Tiles tiles_for(const pqc_paged_config* c, const Geometry& g, const int* offsets) {
   if (!offsets) return Tiles::kOne;

@@ -127,8 +127,8 @@ __device__ __forceinline__ Item find_item(const Geometry& g, const int* lengths,
 
 // The kernel of 16 rows, which waits for bytes: all tiles of a head laid end to end, one per query tile of every sequence, a tile
 // being its sequence's tokens in units of `grain` and kTileCost units in front of them for what a tile costs by itself.  Every
-// worker of the head takes the same share of units, wherever that begins and ends, so that the workgroups, which are all
-// resident at once, end together: 48 ragged sequences of 8 heads as whole splits over 512 workgroups took 80 us.  A border inside a
+// worker of the head takes the same share of units, wherever that begins and ends (the quotient rounded up, so that of few units the last workers
+// have none), so that the workgroups, which are all resident at once, end about together: 48 ragged sequences of 8 heads as whole splits over 512 workgroups took 80 us.  A border inside a
 // tile's first kTileCost units counts as its beginning.
 constexpr int kTileCost = 2;
 struct Border {
