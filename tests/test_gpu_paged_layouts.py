@@ -109,3 +109,122 @@ MANY_SEQUENCES = {  # lengths, queries, P, heads, G, D, cache, dtype, out
 @pytest.mark.parametrize("case", MANY_SEQUENCES)
 def test_several_tokens_of_many_sequences(paged, case):
     base.test_attention_of_several_tokens(paged, *MANY_SEQUENCES[case])
+
+
+# ------------------------------------------------------------------ what the documentation allows beside the ordinary
+def test_offsets_that_begin_behind_the_first_row(paged):
+    gen = torch.Generator().manual_seed(12)
+    P, heads, G, D, n = 16, 2, 2, 64, 80
+    off = torch.tensor([3, 3, 40, 71], dtype=torch.int32)  # rows 0 .. 2 and from 71 on are nobody's, the first sequence has none
+    lens = torch.tensor([5, 60, 31], dtype=torch.int32)
+    table, n_pages = place(lens.tolist(), P, gen)
+    rotation = paged.rotation_table(64, D, device="cpu")
+    k, v = (ref.fill_pool(n_pages, heads, P, D, "bf16", gen)[0] for _ in range(2))
+    q0, k0, v0 = (torch.randn((n, h, D), generator=gen).to(torch.bfloat16) for h in (heads * G, heads, heads))
+    for t in (q0, k0, v0):
+        t[:3], t[71:] = float("nan"), float("nan")
+    c = paged.PagedCache(dev(k), dev(v), None, None, n_q_heads=heads * G, rotation=dev(rotation))
+    qo, ko = (torch.full_like(dev(t), 7.0) for t in (q0, k0))
+    c.append(dev(k0), dev(v0), dev(table), dev(lens), new_offsets=dev(off), q=dev(q0), q_out=qo, k_out=ko)
+    pos = torch.cat([torch.arange(60 - 37, 60), torch.arange(31)])
+    for got, x in ((qo, q0), (ko, k0)):
+        want = ref.rotated(x[3:71].double(), pos, rotation, "halves")
+        close(got[3:71], want, 2.0 ** -8 * want.abs() + 3 * ref.U * want.abs().amax(-1, keepdim=True))
+        assert bool((got[:3] == 7.0).all()) and bool((got[71:] == 7.0).all())
+    pages = (c.k_pages.cpu(), c.v_pages.cpu(), None, None)
+    want_k, _, tol = ref.append(ref.rotated(torch.cat([torch.zeros(3, heads, D), k0[3:71].float()]).double(), torch.cat([torch.zeros(3).long(), pos]), rotation, "halves"), k, None, table, lens, off)
+    assert bool(((ref.dequantised(pages[0], None) - want_k).abs() <= tol).all())
+    # the wide tiles, and those of 16 rows with queries for the last places only
+    for several in (off, torch.tensor([2, 2, 5, 9], dtype=torch.int32)):
+        rows = int(several[-1]) + 4
+        q = torch.randn((rows, heads * G, D), generator=gen).to(torch.bfloat16)
+        q[:int(several[0])], q[int(several[-1]):] = float("nan"), float("nan")
+        out = torch.full((rows, heads * G, D), 7.0, device=DEV)
+        c.attn(dev(q), dev(table), dev(lens), q_offsets=dev(several), out=out)
+        want, tol = ref.attention(q, pages, table, lens, several, D ** -0.5, "f32")
+        close(out, want, tol)
+        lo, hi = int(several[0]), int(several[-1])
+        assert bool((out[:lo] == 7.0).all()) and bool((out[hi:] == 7.0).all())
+
+
+def test_tokens_taken_back(paged):
+    """A program that drafts tokens and rejects some: shorter lengths, then other tokens in their places.  What stays is as it was."""
+    gen = torch.Generator().manual_seed(13)
+    P, heads, D = 16, 2, 64
+    c = paged.PagedCache.empty(4, 4, heads, D, P, device=DEV)
+    table = torch.tensor([[2, 0, 3]], dtype=torch.int32)
+    lens = lambda n: torch.tensor([n], dtype=torch.int32, device=DEV)  # noqa: E731
+    x = torch.randn((40, heads, D), generator=gen).to(torch.bfloat16)
+    kept, at = [], 0
+    for new, stay, size in ((14, 14, 1.0), (5, 2, 8.0), (4, 1, 1.0), (5, 5, 0.25), (6, 3, 2.0)):
+        t = dev((x[at:at + new].float() * size).to(torch.bfloat16))
+        at += new
+        n = len(kept) + new
+        c.append(t, t, dev(table), lens(n), new_offsets=torch.tensor([0, new], dtype=torch.int32, device=DEV))
+        kept += list(t[:stay].cpu())
+    want = torch.stack(kept).double()
+    n = len(kept)
+    for pool, scale in ((c.k_pages, c.k_scale), (c.v_pages, c.v_scale)):
+        got = ref.dequantised(pool.cpu(), scale.cpu())[table[0].long()].transpose(1, 2).reshape(-1, heads, D)[:n]
+        s = scale.cpu()[table[0].long()].double().repeat_interleave(P, 0)[:n, :, None]
+        assert bool(((got - want).abs() <= 2.0 ** -4 * want.abs() + 2.0 ** -9 * s).all())
+    q = torch.randn((1, 4, D), generator=gen).to(torch.bfloat16)
+    pages = tuple(t.cpu() for t in (c.k_pages, c.v_pages, c.k_scale, c.v_scale))
+    close(c.attn(dev(q), dev(table), lens(n)), *ref.attention(q, pages, table, torch.tensor([n]), None, D ** -0.5, "f32"))
+
+
+def test_rotated_keys_without_a_place(paged):
+    # more new tokens than the length says, or than the table has room for: their queries are rotated, their keys' rows are left
+    x = torch.randn((9, 1, 64), generator=torch.Generator().manual_seed(14)).to(torch.bfloat16)
+    rotation = paged.rotation_table(40, 64, device="cpu")
+    c = paged.PagedCache.empty(2, 1, 1, 64, 16, "bf16", device=DEV, rotation=dev(rotation))
+    off = torch.tensor([0, 4, 9], dtype=torch.int32, device=DEV)
+    ko = torch.full((9, 1, 64), 7.0, dtype=torch.bfloat16, device=DEV)
+    table, lens = torch.tensor([[0], [1]], dtype=torch.int32, device=DEV), torch.tensor([2, 18], dtype=torch.int32, device=DEV)
+    qo = c.append(dev(x), dev(x), table, lens, new_offsets=off, q=dev(x), k_out=ko)
+    pos = torch.tensor([-2, -1, 0, 1, 13, 14, 15, 16, 17]).clamp(min=0)
+    want = ref.rotated(x.double(), pos, rotation, "halves")
+    tol = 2.0 ** -8 * want.abs() + 3 * ref.U * want.abs().amax(-1, keepdim=True)
+    close(qo, want, tol)
+    close(ko[2:7], want[2:7], tol[2:7])
+    assert bool((ko[:2] == 7.0).all()) and bool((ko[7:] == 7.0).all())
+
+
+@pytest.mark.parametrize("heads", [200, 300, 600])
+def test_hundreds_of_heads(paged, heads):
+    # fewer workgroups per head than parts could be folded by, down to one
+    base.test_attention_of_one_token(paged, [300, 5, 17], 16, heads, 1, 64, "fp8", "bf16", "f32")
+    base.test_attention_of_several_tokens(paged, [200, 31], [3, 4], 16, heads, 2, 64, "bf16", "bf16", "f32")
+    base.test_attention_of_several_tokens(paged, [600, 70], [70, 66], 32, heads, 1, 64, "fp8", "bf16", "bf16")
+    base.test_attention_to_listed_tokens(paged, [300, 90], 150, 16, heads, 1, 64, "fp8", "bf16", "f32")
+    base.test_append(paged, [40, 3], [25, 3], 16, heads, 1, 64, "fp8", "bf16", 64, "halves")
+
+
+def test_thousands_of_sequences_under_a_table_for_16_million_tokens(paged):
+    # units of work are of 512 tokens here, so that their sum stays within 32 bits whatever the lengths; 4.3 GB of page table
+    gen = torch.Generator().manual_seed(15)
+    B, P, heads, G, D = 16384, 256, 1, 2, 64
+    lengths = torch.randint(0, 30, (B,), generator=gen).int()
+    long = [(0, 1300), (63, 513), (64, 1024), (9000, 1600), (B - 1, 2000)]
+    for b, t in long:
+        lengths[b] = t
+    n_pages = 64
+    k, ks = ref.fill_pool(n_pages, heads, P, D, "fp8", gen)
+    v, vs = ref.fill_pool(n_pages, heads, P, D, "fp8", gen)
+    own = torch.randint(0, n_pages, (B, 8), generator=gen).int()  # pages are only read: sequences share them
+    table = torch.full((B, 65536), -1, dtype=torch.int32, device=DEV)
+    table[:, :8] = dev(own)
+    c = paged.PagedCache(dev(k), dev(v), dev(ks / 64.0), dev(vs), n_q_heads=heads * G)
+    q = torch.randn((B, heads * G, D), generator=gen).to(torch.bfloat16)
+    some = [b for b, _ in long] + [1, 62, 65, 127, 128, 5000, B - 2]
+    got = c.attn(dev(q), table, dev(lengths))
+    few = 3 * torch.arange(B + 1, dtype=torch.int32)
+    q3 = torch.randn((3 * B, heads * G, D), generator=gen).to(torch.bfloat16)
+    got3 = c.attn(dev(q3), table, dev(lengths), q_offsets=dev(few))
+    torch.cuda.synchronize()
+    pages = (k, v, ks / 64.0, vs)
+    for b in some:
+        one = (own[b:b + 1], lengths[b:b + 1])
+        close(got[b:b + 1], *ref.attention(q[b:b + 1], pages, *one, None, D ** -0.5, "f32"), f"sequence {b}")
+        close(got3[3 * b:3 * b + 3], *ref.attention(q3[3 * b:3 * b + 3], pages, *one, torch.tensor([0, 3]), D ** -0.5, "f32"), f"queries of {b}")
+    assert bool((got[dev(lengths) == 0] == 0).all())
