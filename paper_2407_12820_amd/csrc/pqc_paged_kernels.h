@@ -1026,13 +1026,14 @@ __global__ __launch_bounds__(256) void attn_block_fold_kernel(Geometry g, const 
 // TERMS: bf16 terms of a weight: three, which is all of it, for an fp32 output, two for a bf16 output (2^-17 of a weight, of the output's own
 // rounding a 512th).  One, 2^-8, moves a bf16 output by as much again as its rounding does: prompts of 8192 tokens 2.1e-3 off 64 bits,
 // with two 1.63e-3, which is the rounding alone, for 1.3 times the time.
-// The vector ALU has about as much to do as the matrix cores (64 tokens, one wave: 32 exponentials and some 300 other instructions
-// against 48 matrix instructions of 32 cycles), so the two run side by side within a wave: the weights of a round's tokens
+// The vector ALU has as much to do as the matrix cores (64 tokens, one wave: 32 exponentials and some 300 other instructions against 48
+// matrix instructions of 32 cycles; busy 57 % and 49 % of the time), so the two run side by side within a wave: the weights of a round's tokens
 // are computed while the values of the round before are multiplied, keys being a round ahead of values.  Two workgroups share a compute
-// unit (one alone takes 1.4 times as long).  Prompts of 8192 tokens, 32 query heads, 8 KV heads: 757 us, 726 TFLOP/s, for an fp32
-// output 931.  (Measured with one term, 581 us: round after round without the overlap 634; operands read one instruction ahead instead of
-// four 604.)  Splitting weights into terms as they are computed instead of in front of their product: 766.  64 rows per wave, which
-// would halve the reads of LDS, need more registers than the vector ALU reaches and spend the gain on copies.
+// unit (one alone takes 1.4 times as long).  Prompts of 8192 tokens, 32 query heads, 8 KV heads: 757 to 799 us over several runs, 688 to 726
+// TFLOP/s; for an fp32 output 900 to 976.  (Measured with one term, 581 us: round after round without the overlap 634; operands read one
+// instruction ahead instead of four 604.)  Splitting weights into terms as they are computed instead of in front of their product took 766
+// against 757.  64 rows per wave, which would halve the reads of LDS, need more registers than the vector ALU reaches and spend the gain on copies.
+// Of that time 1.5 % are for scales that may be no powers of two.
 template <typename T, class C, int D, int TERMS>
 __global__ __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) void attn_block_kernel(Geometry g, Cache c, const T* __restrict__ q,
                                                                                             const int* __restrict__ offsets,
