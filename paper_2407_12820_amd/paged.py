@@ -79,11 +79,15 @@ class _Device:
         self.streams, self.spare = {}, []
         self.recorded = {}  # by recording and raw stream: its graph's for good, 2 KB each
 
-    def stream(self, raw: int, device) -> _Scratch:
-        """For a call that runs now, which also sees to counters for the recordings to come."""
+    def restock(self, device) -> None:
+        """Counters for recordings to come, if there are none."""
         if not self.spare:
             self.spare = list(torch.zeros((self.SPARE, self.WORDS), dtype=torch.int32, device=device))
             torch.cuda.current_stream(device).synchronize()  # a graph may run on any stream
+
+    def stream(self, raw: int, device) -> _Scratch:
+        """For a call that runs now."""
+        self.restock(device)
         found = self.streams.get(raw)
         if found is None:
             found = self.streams[raw] = _Scratch(device, self.WORDS)
@@ -119,7 +123,7 @@ class PagedCache:
     rotation_table() or one laid out like it, None for no rotation.  Like a decode context it is not thread-safe.
 
     Calls run on the current stream, or on `stream`, to which their allocations then belong too.  They may be recorded into
-    graphs; make one ordinary attention call before, so that the counters that save a launch exist."""
+    graphs."""
 
     def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, k_scale: Optional[torch.Tensor], v_scale: Optional[torch.Tensor], *,
                  n_q_heads: int, dtype: str = "bf16", out_dtype: str = "f32", softmax_scale: float = 0.0,
@@ -154,6 +158,10 @@ class PagedCache:
         self._scratch = _devices.setdefault(self._dev, _Device())
         self._counted = 0 < self.lib.pqc_paged_counter_bytes(self._cfg) <= 4 * _Device.WORDS
         self._sizes = {}  # workspace bytes by (query tokens, listed tokens, batch, max_pages)
+        if self._dev >= 0:
+            with _lock, torch.cuda.device(self._dev):
+                if not torch.cuda.is_current_stream_capturing():
+                    self._scratch.restock(self.device)
         self._set = (1, 1, None, None, None)  # batch, max_pages, page table, lengths and counters as they are in the structures
 
     @classmethod
@@ -261,7 +269,8 @@ class PagedCache:
     def append(self, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor, *, new_offsets=None, q=None,
                positions=None, q_out=None, k_out=None, stream=None):
         """New tokens k, v [n][Hkv][D] (rows of a projection allowed) join their sequences; `lengths` counts them already.
-        With q [n][Hq][D] returns its rotated copy (q_out if given); k_out, if given, receives the rotated keys."""
+        With q [n][Hq][D] returns its rotated copy (q_out if given); k_out, if given, receives the rotated keys of the tokens that have a
+        place in the table.  Outputs over each other, an input or the pages are refused."""
         if stream is not None:
             self._own(stream)
             with torch.cuda.stream(stream):

@@ -79,3 +79,24 @@ def test_ordinary_calls_make_room_for_more_recordings(paged):
     assert count_launches(lambda: step()) == 2
     held = {t.data_ptr() for t in kept + c._scratch.spare}
     assert len(held) == len(kept) + len(c._scratch.spare)
+
+
+def test_a_first_call_may_be_recorded(paged):
+    # a device that no cache was made on before: the counters are there with the cache, not with its first ordinary call
+    known = paged._devices.pop(torch.cuda.current_device(), None)
+    try:
+        c, step = call_of(paged)
+        left = len(c._scratch.spare)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            res = step()
+        assert left > 0 and len(c._scratch.spare) == left - 1 and not c._scratch.streams
+        for _ in range(3):
+            graph.replay()
+            want = step()
+            torch.cuda.synchronize()
+            for a, b in zip(res, want):
+                assert torch.equal(a, b)
+    finally:
+        if known is not None:
+            paged._devices[torch.cuda.current_device()] = known
